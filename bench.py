@@ -101,7 +101,7 @@ def algorithmic_bytes(w, ks, lens=None, rows=1, kv_per_row=None):
 
 # the sources that set what the context passes (the roofline kernels) read and
 # write: their kernels, their launch plan and their arguments
-ROOFLINE_SOURCES = ("vp_attend.hip", "vp_common.h", "vp_internal.h", "vp_plan.hip")
+ROOFLINE_SOURCES = ("vp_attend.hip", "vp_common.h", "vp_internal.h", "vp_plan.hip", "vp_tile.h")
 
 
 def kernel_source_hash(root: str) -> str:
