@@ -324,6 +324,106 @@ vp_status vp_decode_step_static(const vp_shape* shape, const vp_layout* layout, 
                                 void* out, void* stream);
 
 /*
+ * Decoding on a bounded cache
+ * ---------------------------
+ * Two calls beside the method, for the text that it leaves in the cache: the
+ * attention of layers (or steps) that look at a window of it, and the eviction
+ * of rows that attention no longer goes to. A loop that holds its caches to C
+ * rows appends its tokens, calls vp_window_decode_attn with attn_sum, and calls
+ * vp_evict whenever the caches have grown some way past C. Both use shape and
+ * layout as the other calls do (vp_window_decode_attn reads no visual segments
+ * and takes them as NULL).
+ */
+
+/* Which positions the queries see. */
+typedef struct vp_window {
+  int32_t window;   /* W: the query at position p sees (p - W, p]; 0: every position up to p */
+  int32_t n_sink;   /* positions [0, n_sink) stay visible to every query from there on (p >= j still holds) */
+  float sm_scale;   /* logit scale of Z; <= 0 selects 1/sqrt(head_dim) */
+} vp_window;
+
+/* Bytes of device workspace vp_window_decode_attn needs, with attn_sum
+ * (with_sums 1) or without (0). A workspace for more sequences, longer caches or
+ * a larger window is not always large enough for fewer: ask for each shape. */
+vp_status vp_window_workspace_size(const vp_shape* shape, const vp_window* window, int32_t with_sums, size_t* bytes);
+
+/*
+ * vp_window_decode_attn -- attention of the step's T queries over a sliding
+ * window and the first n_sink tokens. Query t is the token at position
+ * p_t = seq_len - T + t and sees the positions j <= p_t with j < n_sink or
+ * j > p_t - W (W = 0: all j <= p_t):
+ *
+ *   Z_{h,j}   = sm_scale * <q_h, K_{g(h), j}>
+ *   out[b, t, h] = sum_j softmax_j(Z_h) V_{g(h), j}                 [B, T, Hq, d]
+ *
+ * A query that sees nothing, or whose logits are all -inf, gives zeros. Rows
+ * that a query does not see have no influence on its output, whatever they hold.
+ * Rows from seq_len on are not read.
+ *
+ * attn_sum (optional, else NULL): float [B, Hkv, max_seq_len], the attention
+ * weight that every cached row has been given. The call adds, for every row
+ * that one of the queries sees, the row's softmax weights of all queries and
+ * all heads of its KV group; rows that none sees, and entries from seq_len on,
+ * are left as they are. The rows of the queries themselves (the last T
+ * positions) are new: their entries start from zero whatever they hold, so a
+ * loop never clears them. The weights are added in a fixed order: the same
+ * call on the same inputs gives the same bits.
+ *
+ * layout: seq_len (and block_table with paged caches); the segments are not
+ * read. shape.max_vis, max_segs, k_cap and scope have no effect. The workspace
+ * must not be shared by concurrent calls.
+ * VP_ERR_RANGE: window < 0, n_sink < 0, sm_scale not finite.
+ */
+vp_status vp_window_decode_attn(const vp_shape* shape, const vp_layout* layout, const vp_window* window,
+                                const void* q, const void* K, const void* V, float* attn_sum, void* out,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/* What vp_evict leaves of a cache. */
+typedef struct vp_evict_params {
+  int32_t budget;    /* C >= 1: rows that a sequence holds at most after the call */
+  int32_t n_sink;    /* first rows that always stay */
+  int32_t n_recent;  /* last rows that always stay; n_sink + n_recent <= budget */
+} vp_evict_params;
+
+/* Bytes of device workspace vp_evict needs. */
+vp_status vp_evict_workspace_size(const vp_shape* shape, const vp_evict_params* params, size_t* bytes);
+
+/*
+ * vp_evict -- eviction from the caches by accumulated attention weight. A
+ * sequence of at most C rows stays as it is. Of a longer one the first n_sink
+ * rows, the last n_recent rows and the C - n_sink - n_recent rows in between
+ * with the largest score stay (ties to the lower position); they move, in their
+ * order, to the rows 0 .. C-1 of K and V, in place.
+ * shape.scope VP_SCOPE_KV_GROUP: every KV head keeps its own rows (U = Hkv kept
+ * lists per sequence), the score being its attn_sum. VP_SCOPE_SEQUENCE: one set
+ * of rows for all KV heads (U = 1), the score being the sum of attn_sum over
+ * the KV heads (added in double, rounded once to float). A NaN sum counts as
+ * the largest.
+ *
+ *   kept         int32 [B*U, C]: positions (before the call) of the rows that
+ *                stay, ascending, then -1
+ *   attn_sum     float [B, Hkv, max_seq_len] (see vp_window_decode_attn)
+ *   attn_sum_out the same layout: row i's sum of the compacted caches, i <
+ *                new_len; later entries are left as they are. May be attn_sum.
+ *   vis_seg_out  NULL, or int32 [n_seg][2] like layout->vis_seg: the segments of
+ *                the compacted sequence (one that lost all its rows has length
+ *                0, which the decode-step calls accept). May be layout->vis_seg.
+ *                VP_SCOPE_SEQUENCE only (VP_ERR_UNSUPPORTED otherwise).
+ *   new_len      int32 [B]: min(seq_len, C). May be layout->seq_len.
+ *
+ * Rows from new_len on, of K, V and attn_sum_out, are left as they are. The
+ * visual segments are read only for vis_seg_out. A block that two sequences
+ * share (or a sequence twice) must not be evicted from: block ids are trusted.
+ * shape.n_queries, max_vis, max_segs and k_cap have no effect on the rows kept.
+ * K and V must be different caches and the workspace must not be shared by
+ * concurrent calls.
+ * VP_ERR_RANGE: budget < 1, n_sink < 0, n_recent < 0, n_sink + n_recent > budget.
+ */
+vp_status vp_evict(const vp_shape* shape, const vp_layout* layout, const vp_evict_params* params,
+                   const float* attn_sum, void* K, void* V, int32_t* kept, float* attn_sum_out,
+                   int32_t* vis_seg_out, int32_t* new_len, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * vp_step_plan -- how vp_visual_mass and vp_decode_step will launch
  * their kernels for this shape (pure host computation; for profiling and
  * benchmarks). flags is a bit set of

@@ -10,6 +10,7 @@
 #include <string>
 #include <vector>
 
+#include "vp_cache.h"
 #include "vp_internal.h"
 
 // Scratch memory of vp_decode_step_static: each GPU the library runs on holds
@@ -300,6 +301,39 @@ MergeArgs merge_args(const vp_shape* s, const Plan& plan, const AttendArgs& a, v
 vp_status check_budget_cap(const vp_shape* s, const vp_params* p) {
   if (s->k_cap < max_budget(s, p))
     return fail(VP_ERR_SHAPE, "k_cap %d < largest budget %d for max_vis %d", s->k_cap, max_budget(s, p), s->max_vis);
+  return VP_OK;
+}
+
+// Host checks and arguments of the bounded-cache calls.
+vp_status check_window(const vp_window* w) {
+  if (!w) return fail(VP_ERR_NULL, "window is NULL");
+  if (w->window < 0) return fail(VP_ERR_RANGE, "window %d < 0", w->window);
+  if (w->n_sink < 0) return fail(VP_ERR_RANGE, "n_sink %d < 0", w->n_sink);
+  if (!std::isfinite(w->sm_scale)) return fail(VP_ERR_RANGE, "sm_scale not finite");
+  return VP_OK;
+}
+
+vp_status check_evict(const vp_evict_params* p) {
+  if (!p) return fail(VP_ERR_NULL, "params is NULL");
+  if (p->budget < 1 || p->budget > kMaxTokens) return fail(VP_ERR_RANGE, "budget %d outside [1, %d]", p->budget, kMaxTokens);
+  if (p->n_sink < 0 || p->n_recent < 0) return fail(VP_ERR_RANGE, "n_sink %d, n_recent %d: negative", p->n_sink, p->n_recent);
+  if (static_cast<int64_t>(p->n_sink) + p->n_recent > p->budget)
+    return fail(VP_ERR_RANGE, "n_sink %d + n_recent %d > budget %d", p->n_sink, p->n_recent, p->budget);
+  return VP_OK;
+}
+
+// sequence lengths, and the block table of paged caches
+vp_status check_rows(const vp_shape* s, const vp_layout* l) {
+  if (!l) return fail(VP_ERR_NULL, "layout is NULL");
+  if (!l->seq_len) return fail(VP_ERR_NULL, "layout seq_len is NULL");
+  if (s->block_size > 0 && !l->block_table) return fail(VP_ERR_NULL, "paged caches (block_size > 0) need a block_table");
+  return VP_OK;
+}
+
+vp_status check_room(void* ws, size_t bytes, size_t need) {
+  if (!ws) return fail(VP_ERR_WORKSPACE, "workspace is NULL");
+  if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return fail(VP_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  if (bytes < need) return fail(VP_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", bytes, need);
   return VP_OK;
 }
 
@@ -668,6 +702,126 @@ vp_status vp_decode_step_static(const vp_shape* shape, const vp_layout* layout, 
   if (vp_status e = static_scratch(&ws)) return e;
   return launch_step(shape, layout, params, plan, static_cast<char*>(ws), q, K, V, mass_head, mass_seq, scores, k,
                      vis_idx, out, static_cast<hipStream_t>(stream), nullptr, 0);
+}
+
+vp_status vp_window_workspace_size(const vp_shape* shape, const vp_window* window, int32_t with_sums, size_t* bytes) {
+  g_last_error.clear();
+  if (vp_status e = check_shape(shape)) return e;
+  if (vp_status e = check_window(window)) return e;
+  if (with_sums != 0 && with_sums != 1) return fail(VP_ERR_RANGE, "with_sums must be 0 or 1");
+  if (!bytes) return fail(VP_ERR_NULL, "bytes is NULL");
+  *bytes = make_window_plan(*shape, *window, with_sums == 1).total;
+  return VP_OK;
+}
+
+vp_status vp_window_decode_attn(const vp_shape* shape, const vp_layout* layout, const vp_window* window, const void* q,
+                                const void* K, const void* V, float* attn_sum, void* out, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+  g_last_error.clear();
+  if (vp_status e = check_shape(shape)) return e;
+  if (vp_status e = check_rows(shape, layout)) return e;
+  if (vp_status e = check_window(window)) return e;
+  if (!q || !K || !V || !out) return fail(VP_ERR_NULL, "q, K, V, out required");
+  if (!aligned16(q) || !aligned16(K) || !aligned16(V) || !aligned16(out))
+    return fail(VP_ERR_SHAPE, "q, K, V, out must be 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(attn_sum) & 3u) return fail(VP_ERR_SHAPE, "attn_sum must be 4-byte aligned");
+  const WindowPlan plan = make_window_plan(*shape, *window, attn_sum != nullptr);
+  if (vp_status e = check_room(workspace, workspace_bytes, plan.total)) return e;
+  char* ws = static_cast<char*>(workspace);
+  WindowArgs a{};
+  a.q = q;
+  a.K = K;
+  a.V = V;
+  a.out = out;
+  a.attn_sum = attn_sum;
+  a.sb = shape->kv_stride_b;
+  a.sh = shape->kv_stride_h;
+  a.ss = shape->kv_stride_s;
+  a.bs_log2 = -1;
+  if (shape->block_size > 0) {
+    a.bs_log2 = __builtin_ctz(static_cast<unsigned>(shape->block_size));
+    a.nblk = (shape->max_seq_len + shape->block_size - 1) / shape->block_size;
+    a.block_table = layout->block_table;
+  }
+  a.seq_len = layout->seq_len;
+  a.B = shape->batch;
+  a.Hq = shape->n_q_heads;
+  a.Hkv = shape->n_kv_heads;
+  a.G = shape->n_q_heads / shape->n_kv_heads;
+  a.T = queries(*shape);
+  a.max_seq_len = shape->max_seq_len;
+  a.window = std::min(window->window, 2 * kMaxTokens);  // (further back than any row)
+  a.n_sink = window->n_sink;
+  const float sm = window->sm_scale > 0.f ? window->sm_scale : 1.0f / std::sqrt(static_cast<float>(shape->head_dim));
+  a.zscale = sm * 1.4426950408889634f;  // log2(e)
+  a.tiles = plan.tiles;
+  a.parts = plan.parts;
+  a.gp = plan.gp;
+  a.stats = reinterpret_cast<float*>(ws + plan.stats);
+  a.acc = reinterpret_cast<float*>(ws + plan.acc);
+  a.zs = reinterpret_cast<float*>(ws + plan.zs);
+  if (hipError_t e = launch_window(a, shape->dtype, shape->head_dim, static_cast<hipStream_t>(stream)))
+    return hip_fail(e, "window attention launch");
+  return VP_OK;
+}
+
+vp_status vp_evict_workspace_size(const vp_shape* shape, const vp_evict_params* params, size_t* bytes) {
+  g_last_error.clear();
+  if (vp_status e = check_shape(shape)) return e;
+  if (vp_status e = check_evict(params)) return e;
+  if (!bytes) return fail(VP_ERR_NULL, "bytes is NULL");
+  *bytes = make_evict_plan(*shape).total;
+  return VP_OK;
+}
+
+vp_status vp_evict(const vp_shape* shape, const vp_layout* layout, const vp_evict_params* params,
+                   const float* attn_sum, void* K, void* V, int32_t* kept, float* attn_sum_out, int32_t* vis_seg_out,
+                   int32_t* new_len, void* workspace, size_t workspace_bytes, void* stream) {
+  g_last_error.clear();
+  if (vp_status e = check_shape(shape)) return e;
+  if (vp_status e = vis_seg_out ? check_layout(shape, layout) : check_rows(shape, layout)) return e;
+  if (vp_status e = check_evict(params)) return e;
+  if (!attn_sum || !K || !V || !kept || !attn_sum_out || !new_len)
+    return fail(VP_ERR_NULL, "attn_sum, K, V, kept, attn_sum_out, new_len required");
+  if (!aligned16(K) || !aligned16(V)) return fail(VP_ERR_SHAPE, "K, V must be 16-byte aligned");
+  if (K == V) return fail(VP_ERR_SHAPE, "K and V are the same cache");
+  if (vis_seg_out && shape->scope != VP_SCOPE_SEQUENCE)
+    return fail(VP_ERR_UNSUPPORTED, "vis_seg_out needs one kept set per sequence (VP_SCOPE_SEQUENCE)");
+  const EvictPlan plan = make_evict_plan(*shape);
+  if (vp_status e = check_room(workspace, workspace_bytes, plan.total)) return e;
+  char* ws = static_cast<char*>(workspace);
+  const int64_t esz = shape->dtype == VP_BF16 ? 2 : 4;
+  EvictArgs a{};
+  a.seq_len = layout->seq_len;
+  a.seg_off = layout->vis_seg_off;
+  a.seg = layout->vis_seg;
+  if (shape->block_size > 0) {
+    a.bs_log2 = __builtin_ctz(static_cast<unsigned>(shape->block_size));
+    a.nblk = (shape->max_seq_len + shape->block_size - 1) / shape->block_size;
+    a.block_table = layout->block_table;
+  }
+  a.B = shape->batch;
+  a.Hkv = shape->n_kv_heads;
+  a.U = rows_per_query(*shape);
+  a.max_seq_len = shape->max_seq_len;
+  a.budget = params->budget;
+  a.n_sink = params->n_sink;
+  a.n_recent = params->n_recent;
+  a.sb = shape->kv_stride_b * esz;
+  a.sh = shape->kv_stride_h * esz;
+  a.ss = shape->kv_stride_s * esz;
+  a.sum = attn_sum;
+  a.sum_out = attn_sum_out;
+  a.K = K;
+  a.V = V;
+  a.kept = kept;
+  a.seg_out = vis_seg_out;
+  a.new_len = new_len;
+  a.meta = reinterpret_cast<int32_t*>(ws + plan.meta);
+  a.keys = reinterpret_cast<uint32_t*>(ws + plan.keys);
+  if (hipError_t e = launch_evict(a, static_cast<int>(shape->head_dim * esz), static_cast<hipStream_t>(stream)))
+    return hip_fail(e, "eviction launch");
+  return VP_OK;
 }
 
 }  // extern "C"

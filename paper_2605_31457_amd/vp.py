@@ -47,6 +47,14 @@ class vp_params(ctypes.Structure):
                 ("r_lo_bp", ctypes.c_int32), ("r_hi_bp", ctypes.c_int32), ("clamp", ctypes.c_int32)]
 
 
+class vp_window(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int32), ("n_sink", ctypes.c_int32), ("sm_scale", ctypes.c_float)]
+
+
+class vp_evict_params(ctypes.Structure):
+    _fields_ = [("budget", ctypes.c_int32), ("n_sink", ctypes.c_int32), ("n_recent", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -75,6 +83,10 @@ def lib() -> ctypes.CDLL:
             "vp_validate_layout": ([P(vp_shape), P(vp_layout), V], ctypes.c_int),
             "vp_decode_step": ([P(vp_shape), P(vp_layout), P(vp_params), V, V, V, V, V, V, V, V, V, V, S, V,
                                 ctypes.POINTER(V), ctypes.c_int32], ctypes.c_int),
+            "vp_window_workspace_size": ([P(vp_shape), P(vp_window), ctypes.c_int32, P(S)], ctypes.c_int),
+            "vp_window_decode_attn": ([P(vp_shape), P(vp_layout), P(vp_window), V, V, V, V, V, V, S, V], ctypes.c_int),
+            "vp_evict_workspace_size": ([P(vp_shape), P(vp_evict_params), P(S)], ctypes.c_int),
+            "vp_evict": ([P(vp_shape), P(vp_layout), P(vp_evict_params), V, V, V, V, V, V, V, V, S, V], ctypes.c_int),
             "vp_stream_read": ([V, S, ctypes.c_int32, V, V], ctypes.c_int),
             "vp_decode_step_static": ([P(vp_shape), P(vp_layout), P(vp_params), V, V, V, V, V, V, V, V, V, V],
                                        ctypes.c_int),
@@ -211,6 +223,40 @@ def vp_sparse_decode_attn(shape, layout, params, q, K, V, vis_idx, k, out, flags
     _check("vp_sparse_decode_attn", lib().vp_sparse_decode_attn(
         ctypes.byref(shape), ctypes.byref(layout), ctypes.byref(params), _p(q), _p(K), _p(V),
         _p(vis_idx), _p(k), _p(out), int(flags), _p(workspace), nbytes, _stream(stream)))
+
+
+def vp_window_workspace_size(shape: vp_shape, window: vp_window, with_sums: bool = False) -> int:
+    n = ctypes.c_size_t(0)
+    _check("vp_window_workspace_size", lib().vp_window_workspace_size(
+        ctypes.byref(shape), ctypes.byref(window), int(with_sums), ctypes.byref(n)))
+    return n.value
+
+
+def vp_window_decode_attn(shape, layout, window, q, K, V, attn_sum, out, workspace, workspace_bytes=None, stream=None):
+    """Attention over a sliding window and the first tokens; attn_sum None, or
+    float32 [B, Hkv, max_seq_len] to which the rows' weights are added."""
+    nbytes = workspace.numel() * workspace.element_size() if workspace_bytes is None else workspace_bytes
+    _check("vp_window_decode_attn", lib().vp_window_decode_attn(
+        ctypes.byref(shape), ctypes.byref(layout), ctypes.byref(window), _p(q), _p(K), _p(V), _p(attn_sum), _p(out),
+        _p(workspace), nbytes, _stream(stream)))
+
+
+def vp_evict_workspace_size(shape: vp_shape, params: vp_evict_params) -> int:
+    n = ctypes.c_size_t(0)
+    _check("vp_evict_workspace_size", lib().vp_evict_workspace_size(
+        ctypes.byref(shape), ctypes.byref(params), ctypes.byref(n)))
+    return n.value
+
+
+def vp_evict(shape, layout, params, attn_sum, K, V, kept, attn_sum_out, vis_seg_out, new_len, workspace,
+             workspace_bytes=None, stream=None):
+    """Keeps the first, the last and the most attended rows of every sequence, in
+    place; vis_seg_out may be None. attn_sum_out, vis_seg_out and new_len may be the
+    arrays that attn_sum and the layout name."""
+    nbytes = workspace.numel() * workspace.element_size() if workspace_bytes is None else workspace_bytes
+    _check("vp_evict", lib().vp_evict(
+        ctypes.byref(shape), ctypes.byref(layout), ctypes.byref(params), _p(attn_sum), _p(K), _p(V), _p(kept),
+        _p(attn_sum_out), _p(vis_seg_out), _p(new_len), _p(workspace), nbytes, _stream(stream)))
 
 
 def vp_validate_layout(shape, layout, stream=None):
