@@ -343,8 +343,9 @@ typedef struct vp_window {
 } vp_window;
 
 /* Bytes of device workspace vp_window_decode_attn needs, with attn_sum
- * (with_sums 1) or without (0). A workspace for more sequences, longer caches or
- * a larger window is not always large enough for fewer: ask for each shape. */
+ * (with_sums 1) or without (0); 0 bytes: none, and NULL will do. A workspace for
+ * more sequences, longer caches or a larger window is not always large enough for
+ * fewer: ask for each shape. */
 vp_status vp_window_workspace_size(const vp_shape* shape, const vp_window* window, int32_t with_sums, size_t* bytes);
 
 /*

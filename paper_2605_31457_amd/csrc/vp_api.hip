@@ -331,6 +331,7 @@ vp_status check_rows(const vp_shape* s, const vp_layout* l) {
 }
 
 vp_status check_room(void* ws, size_t bytes, size_t need) {
+  if (need == 0) return VP_OK;  // (a call that needs none takes NULL)
   if (!ws) return fail(VP_ERR_WORKSPACE, "workspace is NULL");
   if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return fail(VP_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   if (bytes < need) return fail(VP_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", bytes, need);
@@ -755,10 +756,11 @@ vp_status vp_window_decode_attn(const vp_shape* shape, const vp_layout* layout, 
   const float sm = window->sm_scale > 0.f ? window->sm_scale : 1.0f / std::sqrt(static_cast<float>(shape->head_dim));
   a.zscale = sm * 1.4426950408889634f;  // log2(e)
   a.tiles = plan.tiles;
-  a.parts = plan.parts;
+  a.groups = plan.groups;
   a.gp = plan.gp;
   a.stats = reinterpret_cast<float*>(ws + plan.stats);
   a.acc = reinterpret_cast<float*>(ws + plan.acc);
+  a.pieces = reinterpret_cast<int2*>(ws + plan.pieces);
   a.zs = reinterpret_cast<float*>(ws + plan.zs);
   if (hipError_t e = launch_window(a, shape->dtype, shape->head_dim, static_cast<hipStream_t>(stream)))
     return hip_fail(e, "window attention launch");
@@ -770,7 +772,7 @@ vp_status vp_evict_workspace_size(const vp_shape* shape, const vp_evict_params* 
   if (vp_status e = check_shape(shape)) return e;
   if (vp_status e = check_evict(params)) return e;
   if (!bytes) return fail(VP_ERR_NULL, "bytes is NULL");
-  *bytes = make_evict_plan(*shape).total;
+  *bytes = make_evict_plan(*shape, *params).total;
   return VP_OK;
 }
 
@@ -787,7 +789,7 @@ vp_status vp_evict(const vp_shape* shape, const vp_layout* layout, const vp_evic
   if (K == V) return fail(VP_ERR_SHAPE, "K and V are the same cache");
   if (vis_seg_out && shape->scope != VP_SCOPE_SEQUENCE)
     return fail(VP_ERR_UNSUPPORTED, "vis_seg_out needs one kept set per sequence (VP_SCOPE_SEQUENCE)");
-  const EvictPlan plan = make_evict_plan(*shape);
+  const EvictPlan plan = make_evict_plan(*shape, *params);
   if (vp_status e = check_room(workspace, workspace_bytes, plan.total)) return e;
   char* ws = static_cast<char*>(workspace);
   const int64_t esz = shape->dtype == VP_BF16 ? 2 : 4;
@@ -819,6 +821,10 @@ vp_status vp_evict(const vp_shape* shape, const vp_layout* layout, const vp_evic
   a.new_len = new_len;
   a.meta = reinterpret_cast<int32_t*>(ws + plan.meta);
   a.keys = reinterpret_cast<uint32_t*>(ws + plan.keys);
+  a.turns = reinterpret_cast<uint32_t*>(ws + plan.turns);
+  a.rows = plan.rows;
+  a.chunks = plan.chunks;
+  a.turn_words = plan.turn_words;
   if (hipError_t e = launch_evict(a, static_cast<int>(shape->head_dim * esz), static_cast<hipStream_t>(stream)))
     return hip_fail(e, "eviction launch");
   return VP_OK;

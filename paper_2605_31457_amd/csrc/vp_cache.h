@@ -12,11 +12,12 @@ namespace vp {
 // Work decomposition and workspace carving, a pure function of shape and window.
 struct WindowPlan {
   int tiles;     // 32-row tiles that any sequence's queries see, at most
-  int parts;     // work-groups per (sequence, KV head)
+  int groups;    // work-groups that the walks of the batch are dealt to; 0: one per (sequence, KV head)
   int gp;        // floats per spilled row of logits: the query rows padded to 1, 2, 4, 8 or 16
-  size_t stats;  // float [B][Hkv][T*G][parts][2]  per-part (max, sum)
-  size_t acc;    // float [B][Hkv][T*G][parts][d]  per-part value partials
-  size_t zs;     // float [B][Hkv][tiles * 32][gp] logits (log2 domain) by row of the walk
+  size_t stats;  // float [groups][T*G][2]          (max, sum) of each work-group's part of a walk
+  size_t acc;    // float [groups][T*G][d]          its value partials
+  size_t pieces; // int32 [B*Hkv][2]                where a pair's pieces begin, and how many there are
+  size_t zs;     // float [B][Hkv][tiles * 32][gp]  logits (log2 domain) by row of the walk
   size_t total;
 };
 WindowPlan make_window_plan(const vp_shape& s, const vp_window& w, bool sums);
@@ -35,9 +36,10 @@ struct WindowArgs {
   int B, Hq, Hkv, G, T, max_seq_len;
   int window, n_sink;
   float zscale;                // sm_scale * log2(e)
-  int tiles, parts, gp;
+  int tiles, groups, gp;
   float* stats;
   float* acc;
+  int2* pieces;
   float* zs;
 };
 hipError_t launch_window(const WindowArgs& a, int dtype, int head_dim, hipStream_t st);
@@ -81,9 +83,14 @@ struct WindowWalk {
 struct EvictPlan {
   size_t meta;   // int32 [B*U][2]           rows kept, clamped length (of each kept list)
   size_t keys;   // uint32 [B*U][max_seq_len] sort keys, for caches of more rows than registers hold
+  size_t turns;  // uint32 [B*Hkv][turn_words] per KV head: the work-groups that have begun, and one
+                 // word per work-group, set when its rows are read
+  int rows;      // rows per work-group of the move
+  int chunks;    // work-groups that move the rows of a KV head
+  int turn_words;
   size_t total;
 };
-EvictPlan make_evict_plan(const vp_shape& s);
+EvictPlan make_evict_plan(const vp_shape& s, const vp_evict_params& p);
 
 struct EvictArgs {
   const int32_t* seq_len;
@@ -103,6 +110,8 @@ struct EvictArgs {
   int32_t* new_len;            // [B] (may be seq_len)
   int32_t* meta;
   uint32_t* keys;
+  uint32_t* turns;
+  int rows, chunks, turn_words;
 };
 hipError_t launch_evict(const EvictArgs& a, int row_bytes, hipStream_t st);
 

@@ -11,12 +11,19 @@
 //   evict_select_kernel  one 1024-thread work-group per kept list: sort keys of the rows
 //                        in between (registers up to 32768 rows, the workspace beyond),
 //                        radix select and ordered compaction of vp_blocks.h;
-//   evict_move_kernel    the rows. Bound: HBM, every moved row read and written once.
-// Row i comes from kept[i] >= i, so a row is read before it is written over if the
-// rows of lower i are read first: a work-group walks its rows upwards, a step's rows all
-// read before any is written.
+//   evict_move_kernel    the rows, K and V. Bound: HBM, every
+//                        moved row read and written once.
+// Row i comes from kept[i] >= i, in place: it may be written over once the rows that are
+// read from there have been read, and those have lower indices. A work-group reads all of
+// its rows, says so, waits until the work-groups of lower rows have said so and then
+// writes. The work-groups of a KV head take their rows in the order in which they begin
+// (a counter), so what a work-group waits for has begun and waits for nothing before it
+// reads: every wait ends, in whatever order the GPU starts them. (One work-group per KV
+// head and cache that walks its rows upwards, without waits: 1531 us where this takes
+// 441, 32 x 32k tokens, 4 KV heads of 128, to half.)
 #include "vp_blocks.h"
 #include "vp_cache.h"
+#include "vp_tile.h"
 
 namespace vp {
 namespace {
@@ -35,6 +42,36 @@ __device__ __forceinline__ float row_score(const EvictArgs& a, int b, int u, int
   return static_cast<float>(t);
 }
 
+// scores of rows j0, j0 + 64, ... (at most last), the heads outermost: every head's
+// loads are issued together (heads innermost: 40 us for 16 sequences of 12k rows, 4 KV
+// heads, where this takes 17)
+template <int KPT>
+__device__ __forceinline__ void row_scores(const EvictArgs& a, int b, int u, int j0, int last, float (&score)[KPT]) {
+  const float* s = a.sum + (static_cast<size_t>(b) * a.Hkv + u) * a.max_seq_len;
+  if (a.U == a.Hkv) {
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) score[j] = s[min(j0 + 64 * j, last)];
+    return;
+  }
+  constexpr int N = KPT < 16 ? KPT : 16;  // rows in flight
+#pragma unroll
+  for (int c = 0; c < KPT; c += N) {
+    double t[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) t[j] = 0.0;
+    const float* sg = s;
+    for (int g = 0; g < a.Hkv; ++g, sg += a.max_seq_len) {
+      float v[N];
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[j] = sg[min(j0 + 64 * (c + j), last)];
+#pragma unroll
+      for (int j = 0; j < N; ++j) t[j] += static_cast<double>(v[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) score[c + j] = static_cast<float>(t[j]);
+  }
+}
+
 // KPT > 0: the keys in registers (max_seq_len <= KPT * kSelThreads); 0: in the workspace
 template <int KPT>
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictArgs a) {
@@ -51,6 +88,12 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
   if (tid == 0) {
     a.meta[2 * row] = min(L, C);
     a.meta[2 * row + 1] = L;
+  }
+  // the move kernel's counters of this list's KV heads
+  {
+    const int heads = a.U == 1 ? a.Hkv : 1;
+    uint32_t* turns = a.turns + (static_cast<size_t>(b) * a.Hkv + u) * a.turn_words;
+    for (int i = tid; i < heads * a.turn_words; i += kSelThreads) turns[i] = 0u;
   }
   if (L <= C) {
     for (int i = tid; i < C; i += kSelThreads) kept[i] = i < L ? i : -1;
@@ -75,9 +118,11 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
     RegKeys<KPT> keys;
     keys.r0 = wid * 64 * KPT + lane;
     keys.n = n;
+    float score[KPT];
+    row_scores<KPT>(a, b, u, S + keys.r0, S + n - 1, score);
 #pragma unroll
     for (int j = 0; j < KPT; ++j) {  // slots past n hold the last key: no change of the range
-      keys.u[j] = sum_key(row_score(a, b, u, S + min(keys.rank(j), n - 1)));
+      keys.u[j] = sum_key(score[j]);
       kmin = min(kmin, keys.u[j]);
       kmax = max(kmax, keys.u[j]);
     }
@@ -105,77 +150,135 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
 }
 
 constexpr int kMoveThreads = 256;
+// Rows per work-group: 128 KB of K and V (32 x 32k tokens: 64 rows of 256 bytes 627 us, 128 494,
+// 256 441), 32 KB where that would leave CUs idle (1 x 8k tokens: 18.1 us, 256 rows 19.7)
+constexpr int large_rows(int row_bytes) { return row_bytes > 256 ? 128 : 256; }
+constexpr int small_rows(int row_bytes) { return row_bytes > 256 ? 32 : 64; }
 
-// Grid (2 + 1, Hkv, B): the K rows, the V rows, and the sums with (KV head 0) the new
-// length and the segments.
-template <int ROWB>
+// set, or wait for, a word that work-groups of this launch share (device scope: the
+// XCDs' L2 caches are not coherent with each other)
+__device__ __forceinline__ void set_word(uint32_t* p) {
+  __hip_atomic_store(p, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void await_word(const uint32_t* p) {
+  while (__hip_atomic_load(const_cast<uint32_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 0u)
+    __builtin_amdgcn_s_sleep(1);
+}
+
+// 16 bytes of a row that moves: its old place is not read again (cached: 513 us where
+// this takes 494, 32 x 32k tokens at 128 rows per work-group)
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 load_row(const char* p) {
+  const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+  return make_uint4(x.x, x.y, x.z, x.w);
+}
+
+// the visual segments of sequence b in the numbering of its n kept rows (L before)
+__device__ __forceinline__ void move_segments(const EvictArgs& a, int b, const int32_t* kept, int n, int L, int tid) {
+  __shared__ SegTable tab;
+  const int o0 = a.seg_off[b];
+  if (tid < 64) load_segments(tab, a.seg + 2 * static_cast<long>(o0), a.seg_off[b + 1] - o0, L, tid);
+  __syncthreads();
+  // rows kept before position p
+  auto before = [&](int p) {
+    int lo = 0, hi = n;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (kept[mid] < p) lo = mid + 1;
+      else hi = mid;
+    }
+    return lo;
+  };
+  for (int s = tid; s < tab.n; s += kMoveThreads) {
+    const int st = before(tab.st[s]), en = before(tab.en[s]);
+    a.seg_out[2 * (static_cast<long>(o0) + s)] = st;
+    a.seg_out[2 * (static_cast<long>(o0) + s) + 1] = en - st;
+  }
+}
+
+// Grid (chunks, Hkv, B), and one more work-group per KV head when segments are wanted.
+template <int ROWB, int ROWS>
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(const EvictArgs a) {
-  const int what = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
+  constexpr int PIECES = ROWB / 16;
+  constexpr int RPR = kMoveThreads / PIECES;  // rows per round of loads
+  constexpr int U = ROWS / RPR;          // rounds
+  static_assert(U * RPR == ROWS && ROWS <= kMoveThreads, "rows of a work-group");
+  __shared__ int s_turn;
+  __shared__ int s_src[ROWS];  // position each row comes from (its own: it stays; -1: no row)
+  __shared__ size_t s_from[ROWS], s_to[ROWS];
+  const int g = blockIdx.y, b = blockIdx.z;
   const int tid = threadIdx.x;
   const int row = b * a.U + (a.U == 1 ? 0 : g);
+  uint32_t* turns = a.turns + (static_cast<size_t>(b) * a.Hkv + g) * a.turn_words;
+  if (tid == 0)
+    s_turn = static_cast<int>(__hip_atomic_fetch_add(turns, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
   const int n = a.meta[2 * row], L = a.meta[2 * row + 1];
   const int32_t* kept = a.kept + static_cast<size_t>(row) * a.budget;
-  if (what == 2) {
-    const float* src = a.sum + (static_cast<size_t>(b) * a.Hkv + g) * a.max_seq_len;
-    float* dst = a.sum_out + (static_cast<size_t>(b) * a.Hkv + g) * a.max_seq_len;
-    for (int i0 = 0; i0 < n; i0 += kMoveThreads) {
-      const int i = i0 + tid;
-      const float v = i < n ? src[kept[i]] : 0.f;
-      __syncthreads();
-      if (i < n) dst[i] = v;
-    }
-    if (g != 0) return;
-    if (tid == 0) a.new_len[b] = n;
-    if (!a.seg_out) return;
-    __shared__ SegTable tab;
-    const int o0 = a.seg_off[b];
-    if (tid < 64) load_segments(tab, a.seg + 2 * static_cast<long>(o0), a.seg_off[b + 1] - o0, L, tid);
-    __syncthreads();
-    // rows kept before position p
-    auto before = [&](int p) {
-      int lo = 0, hi = n;
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (kept[mid] < p) lo = mid + 1;
-        else hi = mid;
-      }
-      return lo;
-    };
-    for (int s = tid; s < tab.n; s += kMoveThreads) {
-      const int st = before(tab.st[s]), en = before(tab.en[s]);
-      a.seg_out[2 * (static_cast<long>(o0) + s)] = st;
-      a.seg_out[2 * (static_cast<long>(o0) + s) + 1] = en - st;
-    }
+  __syncthreads();
+  const int c = s_turn;
+  if (c == a.chunks) {
+    if (g == 0) move_segments(a, b, kept, n, L, tid);
     return;
   }
-  constexpr int PIECES = ROWB / 16;
-  constexpr int RPS = kMoveThreads / PIECES;  // rows per round of loads
-  constexpr int U = 8;                        // rounds per step
-  char* base = static_cast<char*>(what == 0 ? a.K : a.V);
-  const int32_t* bt = a.block_table ? a.block_table + static_cast<size_t>(b) * a.nblk : nullptr;
-  const int bmask = (1 << a.bs_log2) - 1;
-  auto at = [&](int j) -> uint4* {
-    const size_t off = bt ? static_cast<size_t>(bt[j >> a.bs_log2]) * a.sb + static_cast<size_t>(j & bmask) * a.ss
-                          : static_cast<size_t>(b) * a.sb + static_cast<size_t>(j) * a.ss;
-    return reinterpret_cast<uint4*>(base + off + static_cast<size_t>(g) * a.sh) + tid % PIECES;
-  };
-  for (int i0 = 0; i0 < n; i0 += RPS * U) {
-    uint4 v[U];
-    int src[U];
-#pragma unroll
-    for (int j = 0; j < U; ++j) {
-      const int i = i0 + j * RPS + tid / PIECES;
-      src[j] = i < n ? kept[i] : -1;
-      if (src[j] != i && i < n) v[j] = *at(src[j]);
+  if (c == 0 && g == 0 && tid == 0) a.new_len[b] = n;
+  const int i0 = c * ROWS;
+  if (i0 >= n) return;  // (rows past the end are nobody's source)
+  const int64_t head = static_cast<int64_t>(g) * a.sh;
+  float sum = 0.f;
+  const size_t sums = (static_cast<size_t>(b) * a.Hkv + g) * a.max_seq_len;
+  if (tid < ROWS) {
+    const int i = i0 + tid;
+    const int src = i < n ? kept[i] : -1;
+    const int from = src < 0 ? 0 : src, to = i < n ? i : 0;
+    if (a.block_table) {
+      const int32_t* bt = a.block_table + static_cast<size_t>(b) * a.nblk;
+      const int mask = (1 << a.bs_log2) - 1;
+      s_from[tid] = static_cast<size_t>(bt[from >> a.bs_log2]) * a.sb + static_cast<size_t>(from & mask) * a.ss + head;
+      s_to[tid] = static_cast<size_t>(bt[to >> a.bs_log2]) * a.sb + static_cast<size_t>(to & mask) * a.ss + head;
+    } else {
+      s_from[tid] = static_cast<size_t>(b) * a.sb + static_cast<size_t>(from) * a.ss + head;
+      s_to[tid] = static_cast<size_t>(b) * a.sb + static_cast<size_t>(to) * a.ss + head;
     }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < U; ++j) {
-      const int i = i0 + j * RPS + tid / PIECES;
-      if (src[j] != i && i < n) *at(i) = v[j];
-    }
-    __syncthreads();
+    s_src[tid] = src;
+    if (src >= 0) sum = a.sum[sums + src];
   }
+  __syncthreads();
+  const int r0 = tid / PIECES;
+  const size_t piece = 16 * static_cast<size_t>(tid % PIECES);
+  uint4 k[U], v[U];
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const int r = j * RPR + r0;
+    k[j] = v[j] = make_uint4(0u, 0u, 0u, 0u);
+    if (s_src[r] > i0 + r) {
+      k[j] = load_row(static_cast<const char*>(a.K) + s_from[r] + piece);
+      v[j] = load_row(static_cast<const char*>(a.V) + s_from[r] + piece);
+    }
+  }
+  // the rows and the sums are in registers: what follows waits for every load
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    unhoist_vector(k[j].x);
+    unhoist_vector(v[j].x);
+  }
+  unhoist_vector(sum);
+  __syncthreads();
+  if (tid == 0) set_word(turns + 1 + c);
+  // Rows of this chunk may be the source of chunks that began earlier: at most L - n
+  // rows further down. Each of those has begun, and sets its word without waiting for
+  // anything, so the wait ends.
+  const int lowest = max(0, i0 - (L - n)) / ROWS;
+  for (int w = lowest + tid; w < c; w += kMoveThreads) await_word(turns + 1 + w);
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const int r = j * RPR + r0;
+    if (s_src[r] > i0 + r) {
+      *reinterpret_cast<uint4*>(static_cast<char*>(a.K) + s_to[r] + piece) = k[j];
+      *reinterpret_cast<uint4*>(static_cast<char*>(a.V) + s_to[r] + piece) = v[j];
+    }
+  }
+  if (tid < ROWS && i0 + tid < n) a.sum_out[sums + i0 + tid] = sum;
 }
 
 template <int KPT>
@@ -185,12 +288,16 @@ void launch_select_keys(const EvictArgs& a, hipStream_t st) {
 
 template <int ROWB>
 void launch_move(const EvictArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((evict_move_kernel<ROWB>), dim3(3, a.Hkv, a.B), dim3(kMoveThreads), 0, st, a);
+  const dim3 grid(a.chunks + (a.seg_out ? 1 : 0), a.Hkv, a.B);
+  if (a.rows == large_rows(ROWB))
+    hipLaunchKernelGGL((evict_move_kernel<ROWB, large_rows(ROWB)>), grid, dim3(kMoveThreads), 0, st, a);
+  else
+    hipLaunchKernelGGL((evict_move_kernel<ROWB, small_rows(ROWB)>), grid, dim3(kMoveThreads), 0, st, a);
 }
 
 }  // namespace
 
-EvictPlan make_evict_plan(const vp_shape& s) {
+EvictPlan make_evict_plan(const vp_shape& s, const vp_evict_params& e) {
   auto align = [](size_t x) { return (x + 255) & ~static_cast<size_t>(255); };
   EvictPlan p{};
   const size_t rows = static_cast<size_t>(s.batch) * rows_per_query(s);
@@ -199,6 +306,14 @@ EvictPlan make_evict_plan(const vp_shape& s) {
   off = align(off + rows * 2 * 4);
   p.keys = off;
   if (reg_keys(s.max_seq_len) == 0) off = align(off + rows * s.max_seq_len * 4);
+  p.turns = off;
+  const int most = e.budget < s.max_seq_len ? e.budget : s.max_seq_len;  // rows a sequence holds afterwards
+  const int row_bytes = s.head_dim * (s.dtype == VP_BF16 ? 2 : 4);
+  p.rows = large_rows(row_bytes);
+  if (static_cast<int64_t>(s.batch) * s.n_kv_heads * ((most + p.rows - 1) / p.rows) < 256) p.rows = small_rows(row_bytes);
+  p.chunks = (most + p.rows - 1) / p.rows;
+  p.turn_words = (1 + p.chunks + 31) / 32 * 32;  // (KV heads on cache lines of their own)
+  off = align(off + static_cast<size_t>(s.batch) * s.n_kv_heads * p.turn_words * 4);
   p.total = off;
   return p;
 }

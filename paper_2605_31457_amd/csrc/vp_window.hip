@@ -10,18 +10,22 @@
 // dependent loads.
 //
 // Two kernels:
-//   window_kernel  one pass over the rows with a running maximum and sum. Grid (parts,
-//                  Hkv, B); the four waves of a work-group take 32-row tiles of the
-//                  walk (WindowWalk) in turn, part p's wave w the tiles p + parts * w,
-//                  p + parts * (w + 4), ...: consecutive work-groups, so all XCDs, read
-//                  consecutive tiles. The T*G <= 16 query rows of the KV head share
-//                  every tile. The waves' partials meet in LDS; a KV head with one part
-//                  is finished there. With sums the logits leave as rows of gp floats
-//                  (32 bytes per row at 7 heads, beside 512 bytes of K and V), since a
-//                  weight is known only when the whole walk is.
-//   finish_kernel  joins the parts of each head, and turns the logits into weights:
+//   window_kernel  one pass over the rows with a running maximum and sum. Every (sequence,
+//                  KV head) pair has work-groups in proportion to the 32-row tiles of its
+//                  walk (WindowWalk), as many as are resident at a time in all, so that
+//                  ragged lengths leave no CU idle; every work-group finds its pair and part
+//                  from the lengths (Deal). A part is a run of consecutive tiles, which
+//                  its four waves take in turn (dealt out cyclically, the parts of 16
+//                  contexts of 32k tokens walk their caches in step, 8 MB apart: 200 us
+//                  where runs take 158); the T*G <= 16 query rows of the KV head share
+//                  every tile. The waves' partials meet in LDS. With
+//                  sums the logits leave as rows of gp floats (32 bytes per row at 7 heads,
+//                  beside 512 bytes of K and V), since a weight is known only when the
+//                  whole walk is.
+//   finish_kernel  joins the pieces of each query row, and turns the logits into weights:
 //                  one thread per row, the query rows in order, so the sums do not
 //                  depend on the partition of the walk or on arrival.
+// Short walks, and those of very many pairs, have one work-group per pair, which does both.
 //
 // A masked row weighs nothing whatever it holds: its logit is not looked at, and in
 // the tiles where some query does not see some row (the ends of the window, of the
@@ -29,6 +33,7 @@
 // replaced by zeros, so that a NaN or infinity there stays out of its output.
 #include <algorithm>
 
+#include "vp_blocks.h"
 #include "vp_cache.h"
 #include "vp_tile.h"
 
@@ -39,6 +44,13 @@ constexpr int kWinWaves = 4;
 constexpr int kWinThreads = 64 * kWinWaves;
 
 size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
+
+#ifndef VP_ONE_GROUP_TILES
+#define VP_ONE_GROUP_TILES 8  // walks of up to this many tiles: one work-group each, no second launch
+#endif
+#ifndef VP_ONE_GROUP_PAIRS
+#define VP_ONE_GROUP_PAIRS 2048  // from this many (sequence, KV head) pairs on too
+#endif
 
 // A running maximum is raised only when a logit exceeds it by more than this (log2
 // units): weights stay below 2^64, and rescaling is rare
@@ -74,6 +86,162 @@ __device__ __forceinline__ size_t out_row(const WindowArgs& a, int b, int g, int
   return (static_cast<size_t>(b) * a.T + r / a.G) * a.Hq + g * a.G + r % a.G;
 }
 
+__device__ __forceinline__ WindowWalk walk_of(const WindowArgs& a, int b) {
+  return WindowWalk(clamp_len(a.seq_len[b], a.max_seq_len), a.T, a.window, a.n_sink);
+}
+
+// How the walks of a batch are dealt to `groups` work-groups, found by every wave from
+// the lengths (no barrier): a work-group takes about `share` tiles of one pair, so a pair
+// of n tiles has ceil(n / share) of them, its parts. Up to 64 sequences have a lane each,
+// one load of the lengths is all that is read, and share is the least multiple of a
+// round of the four waves whose work-groups are not too many; more sequences have
+// consecutive ones in every lane, and share is what always fits.
+struct Deal {
+  int b, g, part, parts;  // this work-group's sequence, KV head and part of parts; b < 0: none
+  int L;                  // the sequence's length
+  __device__ __forceinline__ Deal(const WindowArgs& a, int lane, int group) {
+    const int per = (a.B + 63) / 64;
+    const int i0 = lane * per, i1 = min(a.B, i0 + per);
+    int len = 0, mine = 0;  // of a lane's sequences: the (one) length, their tiles
+    if (per == 1) {
+      len = i0 < i1 ? clamp_len(a.seq_len[i0], a.max_seq_len) : 0;
+      mine = tiles(a, len);
+    } else {
+      mine = sum(a, i0, i1, [](int n) { return n; });
+    }
+    const int total = a.Hkv * __builtin_amdgcn_readlane(wave_incl_sum(mine), 63);
+    const int pairs = a.Hkv * a.B;
+    int share = max(1, (total + a.groups - 1) / a.groups), count = 0;
+    share = (share + kWinWaves - 1) / kWinWaves * kWinWaves;
+    if (per == 1) {
+      // (ends: a share of the longest walk gives every pair one part, and there are as many groups)
+      for (;; share += max(1, share / 128) * kWinWaves) {
+        count = wave_incl_sum(split(mine, share));
+        if (a.Hkv * __builtin_amdgcn_readlane(count, 63) <= a.groups) break;
+      }
+      mine = split(mine, share);
+    } else {
+      share = max(share, (total + a.groups - pairs - 1) / (a.groups - pairs));
+      mine = sum(a, i0, i1, [&](int n) { return split(n, share); });
+      count = wave_incl_sum(mine);
+    }
+    // count: parts of this lane's sequences and those before, for one KV head
+    const bool here = a.Hkv * (count - mine) <= group && group < a.Hkv * count;
+    const uint64_t found = __builtin_amdgcn_ballot_w64(here);
+    b = -1;
+    if (found == 0) return;
+    const int src = __builtin_ctzll(found);
+    int before = count - mine, at = i0, own = mine;
+    if (per > 1 && here) {
+      for (own = split(walk_of(a, at).n, share); group >= a.Hkv * (before + own); own = split(walk_of(a, at).n, share)) {
+        before += own;
+        ++at;
+      }
+    }
+    b = __builtin_amdgcn_readlane(at, src);
+    parts = __builtin_amdgcn_readlane(own, src);
+    const int i = group - a.Hkv * __builtin_amdgcn_readlane(before, src);
+    g = i / parts;
+    part = i - g * parts;
+    L = per == 1 ? __builtin_amdgcn_readlane(len, src) : clamp_len(a.seq_len[b], a.max_seq_len);
+  }
+
+ private:
+  static __device__ __forceinline__ int tiles(const WindowArgs& a, int len) {
+    return WindowWalk(len, a.T, a.window, a.n_sink).n;
+  }
+  static __device__ __forceinline__ int split(int n, int share) {
+    return static_cast<int>((static_cast<unsigned>(n) + share - 1) / static_cast<unsigned>(share));
+  }
+  // f(tiles) over sequences i0 .. i1 - 1, four loads in flight
+  template <typename F>
+  static __device__ __forceinline__ int sum(const WindowArgs& a, int i0, int i1, F f) {
+    int s = 0;
+    for (int i = i0; i < i1; i += 4) {
+      int n[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) n[j] = walk_of(a, min(i + j, a.B - 1)).n;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s += i + j < i1 ? f(n[j]) : 0;
+    }
+    return s;
+  }
+};
+
+// 32 rows at equal steps into an LDS block: those of the tile's lower half from `lower`,
+// the upper half's (TWO; else the same address) from `upper`, both as seen from row 0;
+// row_step holds the lane's offsets of the copies after which they repeat
+template <typename C, int STEPS, bool TWO>
+struct EvenCopy {
+  static __device__ __forceinline__ void rows(const char* lower, const char* upper, const uint32_t (&row_step)[STEPS],
+                                              int rstride, lds_byte* block) {
+    const __amdgpu_buffer_rsrc_t rl =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(lower), 0, 0x7fffffff, kRawBufferWord3);
+    const __amdgpu_buffer_rsrc_t ru =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(upper), 0, 0x7fffffff, kRawBufferWord3);
+#pragma unroll
+    for (int j = 0; j < C::COPIES; ++j)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(TWO && j >= C::COPIES / 2 ? ru : rl, (lds_void*)(block + 1024 * j), 16,
+                                               row_step[j % STEPS], j / STEPS * (STEPS * C::RPI) * rstride, 0,
+                                               kCopyPolicy);
+  }
+};
+
+// a tile's logits, 32 rows of gp floats, from the stage to the plane
+struct StoreLogits {
+  static __device__ __forceinline__ void tile(float* dst, const float* stage, int gp, int lane) {
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+    const u32x4* src = reinterpret_cast<const u32x4*>(stage);
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(dst, 0, 128 * gp, kRawBufferWord3);
+    // (lanes past 128 * gp bytes store nothing)
+    __builtin_amdgcn_raw_buffer_store_b128(src[lane], rs, lane * 16, 0, 0);
+    if (gp > 8) __builtin_amdgcn_raw_buffer_store_b128(src[64 + lane], rs, 1024 + lane * 16, 0, 0);
+  }
+};
+
+// Row i of the walk (tile i / 32) gets its weights of the T*G query rows, in order:
+// norm holds their (max, 1 / sum)
+template <int GP>
+__device__ __forceinline__ void add_weight_gp(const WindowArgs& a, const WindowWalk& w, size_t pair, int i,
+                                              const float2* norm) {
+  const int k = i >> 5;
+  const int j = w.t0(k) + (i & 31);
+  if (j < w.row_begin(k) || j >= w.row_end(k)) return;
+  float z[GP];
+  const float* src = a.zs + (pair * a.tiles * 32 + i) * GP;
+  if constexpr (GP >= 4) {
+#pragma unroll
+    for (int c = 0; c < GP / 4; ++c) {
+      const float4 v = reinterpret_cast<const float4*>(src)[c];
+      z[4 * c] = v.x;
+      z[4 * c + 1] = v.y;
+      z[4 * c + 2] = v.z;
+      z[4 * c + 3] = v.w;
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < GP; ++c) z[c] = src[c];
+  }
+  float* dst = a.attn_sum + pair * a.max_seq_len + j;
+  const float old = j >= w.L - a.T ? 0.f : *dst;
+  float s = 0.f;
+  const int TG = a.T * a.G;
+#pragma unroll
+  for (int h = 0; h < GP; ++h)
+    if (h < TG) s = fmaf(fast_exp2(z[h] - norm[h].x), norm[h].y, s);
+  *dst = old + s;
+}
+__device__ __forceinline__ void add_weight(const WindowArgs& a, const WindowWalk& w, size_t pair, int i,
+                                           const float2* norm) {
+  switch (a.gp) {
+    case 1: add_weight_gp<1>(a, w, pair, i, norm); break;
+    case 2: add_weight_gp<2>(a, w, pair, i, norm); break;
+    case 4: add_weight_gp<4>(a, w, pair, i, norm); break;
+    case 8: add_weight_gp<8>(a, w, pair, i, norm); break;
+    default: add_weight_gp<16>(a, w, pair, i, norm); break;
+  }
+}
+
 template <int DT, int D, bool PAGED, bool SUMS>
 __global__ __launch_bounds__(kWinThreads) __attribute__((amdgpu_waves_per_eu(DT == VP_BF16 ? 2 : 1))) void
 window_kernel(const WindowArgs a) {
@@ -81,22 +249,35 @@ window_kernel(const WindowArgs a) {
   using Q = WinLds<DT, D, SUMS>;
   __shared__ __attribute__((aligned(1024))) unsigned char lds_block[kWinWaves * Q::BYTES];
   __shared__ WinStats ws;
+  __shared__ float2 norm[16];
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const int lane = threadIdx.x & 63;
   const int n16 = lane & 15;
   const int a4 = lane >> 4;
-  const int part = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
   const int TG = a.T * a.G;
   unsigned char* lds = lds_block + wave * Q::BYTES;
   lds_byte* dma = (lds_byte*)lds;
   float* stage = reinterpret_cast<float*>(lds + 2 * C::SUB_ROWS_BYTES);
-
-  // the query rows load while the length arrives
   const bool hv = n16 < TG;
   const int tq = hv ? n16 / a.G : 0;
+
+  const bool dealt = a.groups > 0;
+  int g = blockIdx.y, b = blockIdx.z, part = 0, parts = 1, L;
+  if (dealt) {
+    const Deal deal(a, lane, blockIdx.x);
+    if (deal.b < 0) return;
+    b = deal.b;
+    g = deal.g;
+    part = deal.part;
+    parts = deal.parts;
+    L = deal.L;
+  } else {
+    L = clamp_len(a.seq_len[b], a.max_seq_len);
+  }
+  // the query rows load while the length arrives
   QFrag<DT, D> qf;
   load_q<DT, D>(qf, static_cast<const char*>(a.q) + (hv ? out_row(a, b, g, n16) : 0) * C::ROWB, hv, a4);
-  const WindowWalk w(clamp_len(a.seq_len[b], a.max_seq_len), a.T, a.window, a.n_sink);
+  const WindowWalk w(L, a.T, a.window, a.n_sink);
   const int hi = w.L - a.T + tq;                           // this lane's query sees j <= hi
   const int below = a.window > 0 ? hi - a.window : -1;     // and j > below or j < n_sink
 
@@ -109,28 +290,68 @@ window_kernel(const WindowArgs a) {
   const int bmask = PAGED ? (1 << a.bs_log2) - 1 : 0;
   float* zplane = SUMS ? a.zs + (static_cast<size_t>(b) * a.Hkv + g) * a.tiles * 32 * static_cast<size_t>(a.gp) : nullptr;
 
-  float m = kNoLogit, l = 0.f;  // shared by the four lanes of a query row; l is lane-local
+  // Copies of a tile whose 32 rows are all read: rows at equal steps from one address
+  // (paged caches: from one for each half), so lane offsets that never change. `even`:
+  // the offsets fit 32 bits, and no half of a tile crosses a block.
+  constexpr int STEPS = C::PIECES / C::RPI < C::COPIES ? max_i(C::PIECES / C::RPI, 1) : C::COPIES;
+  const bool even = rstride < (1u << 25) && (!PAGED || bmask >= 15);
+  const int rr = lane / C::PIECES, slot = lane % C::PIECES;
+  uint32_t row_step[STEPS];
+#pragma unroll
+  for (int j = 0; j < STEPS; ++j) {
+    const int r = j * C::RPI + rr;
+    row_step[j] = static_cast<uint32_t>(r) * static_cast<uint32_t>(rstride) + 16 * (slot ^ (r & (C::PIECES - 1)));
+  }
+  // the position read in place of row r of a tile: rows that no query sees are not
+  // read, their places take the nearest row that is read anyway
+  auto row_pos = [&](int t0, int r0, int r1, int r) { return min(max(t0 + r, r0), r1 - 1); };
+  // this part's tiles, and this wave's first one
+  int k = static_cast<int>(static_cast<int64_t>(part) * w.n / parts) + wave;
+  const int k1 = static_cast<int>(static_cast<int64_t>(part + 1) * w.n / parts);
+  // paged caches: lane r < 32 holds the block of row r, loaded a tile ahead
+  auto blocks_of = [&](int k) -> int {
+    int blk = 0;
+    if constexpr (PAGED) {
+      if (k < k1 && lane < 32) blk = bt[row_pos(w.t0(k), w.row_begin(k), w.row_end(k), lane) >> a.bs_log2];
+    }
+    return blk;
+  };
+
+  float m = kNoLogit, l = 0.f;  // m shared by the four lanes of a query row; l lane-local
   f32x4 acc[C::ACC_N];
 #pragma unroll
   for (int i = 0; i < C::ACC_N; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  const int step = a.parts * kWinWaves;
-  for (int k = part + a.parts * wave; k < w.n; k += step) {
+  int blk_next = blocks_of(k);
+  for (; k < k1; k += kWinWaves) {
     const int t0 = w.t0(k);
     const int r0 = w.row_begin(k), r1 = w.row_end(k);  // rows that some query sees, r0 < r1
+    const int blk = blk_next;
     // LDS reads of the previous tile have returned before the copies overwrite it
     __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
-    {
-      // row r of the tile, the others' places take the nearest row that is read anyway
-      const int rr = lane / C::PIECES, slot = lane % C::PIECES;
+    if (even && r0 == t0 && r1 == t0 + 32) {
+      size_t lo, up;
+      if constexpr (PAGED) {
+        lo = static_cast<size_t>(__builtin_amdgcn_readlane(blk, 0)) * bstride + static_cast<size_t>(t0 & bmask) * rstride;
+        up = static_cast<size_t>(__builtin_amdgcn_readlane(blk, 16)) * bstride +
+             static_cast<size_t>((t0 + 16) & bmask) * rstride - 16 * rstride;
+      } else {
+        lo = up = static_cast<size_t>(t0) * rstride;
+      }
+      EvenCopy<C, STEPS, PAGED>::rows(Kb + lo, Kb + up, row_step, static_cast<int>(rstride), dma);
+      EvenCopy<C, STEPS, PAGED>::rows(Vb + lo, Vb + up, row_step, static_cast<int>(rstride), dma + C::SUB_ROWS_BYTES);
+    } else {
+      // (addresses computed here, not kept in registers through the loop)
+      int ln = lane;
+      unhoist_vector(ln);
       size_t off[C::COPIES];
 #pragma unroll
       for (int j = 0; j < C::COPIES; ++j) {
-        const int r = j * C::RPI + rr;
-        const int pos = min(max(t0 + r, r0), r1 - 1);
-        const int piece = 16 * (slot ^ (r & (C::PIECES - 1)));
+        const int r = j * C::RPI + ln / C::PIECES;
+        const int pos = row_pos(t0, r0, r1, r);
+        const int piece = 16 * (ln % C::PIECES ^ (r & (C::PIECES - 1)));
         if constexpr (PAGED)
-          off[j] = static_cast<size_t>(bt[pos >> a.bs_log2]) * bstride + static_cast<size_t>(pos & bmask) * rstride + piece;
+          off[j] = static_cast<size_t>(__shfl(blk, r)) * bstride + static_cast<size_t>(pos & bmask) * rstride + piece;
         else
           off[j] = static_cast<size_t>(pos) * rstride + piece;
       }
@@ -142,6 +363,7 @@ window_kernel(const WindowArgs a) {
         __builtin_amdgcn_global_load_lds((global_void*)(Vb + off[j]), (lds_void*)(dma + C::SUB_ROWS_BYTES + 1024 * j), 16,
                                          0, kCopyPolicy);
     }
+    blk_next = blocks_of(k + kWinWaves);
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
 
     float z[8];
@@ -170,9 +392,7 @@ window_kernel(const WindowArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) stage[pv_token(a4, i) * gp + n16] = (seen >> i) & 1u ? z[i] : kNegInf;
       }
-      const float4* src = reinterpret_cast<const float4*>(stage);
-      float4* dst = reinterpret_cast<float4*>(zplane + static_cast<size_t>(k) * 32 * gp);
-      for (int i = lane; i < 8 * gp; i += 64) dst[i] = src[i];
+      StoreLogits::tile(zplane + static_cast<size_t>(k) * 32 * gp, stage, gp, lane);
     }
     float lmax = kNegInf;
 #pragma unroll
@@ -199,6 +419,9 @@ window_kernel(const WindowArgs a) {
       value_product<DT, D, C::ACC_N, true>(acc, vb, p, a4, n16);
     } else {
       // one query at a time, with the rows that it sees
+      int e4 = a4, e16 = n16;
+      unhoist_vector(e4);
+      unhoist_vector(e16);
 #pragma unroll 1
       for (int t = 0; t < a.T; ++t) {
         const int h = w.L - a.T + t;
@@ -206,14 +429,14 @@ window_kernel(const WindowArgs a) {
         unsigned rows = 0u;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int j = t0 + pv_token(a4, i);
+          const int j = t0 + pv_token(e4, i);
           if (j <= h && (j > lo || j < w.S)) rows |= 1u << i;
         }
         // (a lane's accumulators are its own query row's: those of other queries are dropped)
         f32x4 sum[C::ACC_N];
 #pragma unroll
         for (int i = 0; i < C::ACC_N; ++i) sum[i] = acc[i];
-        value_product<DT, D, C::ACC_N, true, true>(sum, vb, p, a4, n16, rows);
+        value_product<DT, D, C::ACC_N, true, true>(sum, vb, p, e4, e16, rows);
 #pragma unroll
         for (int i = 0; i < C::ACC_N; ++i) acc[i] = tq == t ? sum[i] : acc[i];
       }
@@ -232,6 +455,7 @@ window_kernel(const WindowArgs a) {
   store_acc<DT, D, C::ACC_N>(reinterpret_cast<float*>(lds) + n16 * PITCH, acc, a4);
   __syncthreads();
   const size_t pair = static_cast<size_t>(b) * a.Hkv + g;
+  const size_t piece0 = static_cast<size_t>(blockIdx.x) * TG;
   constexpr int COLS = D / 4;
   for (int i = threadIdx.x; i < TG * COLS; i += kWinThreads) {
     const int h = i / COLS, c = i % COLS;
@@ -250,32 +474,45 @@ window_kernel(const WindowArgs a) {
       o.z = fmaf(f, x.z, o.z);
       o.w = fmaf(f, x.w, o.w);
     }
-    const size_t row = (pair * TG + h) * a.parts + part;
-    if (a.parts == 1) {
-      const float inv = 1.0f / den;
-      const float4 r = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-      store_out<DT>(a.out, out_row(a, b, g, h), D, c, den == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : r);
+    if (dealt) {
+      reinterpret_cast<float4*>(a.acc + (piece0 + h) * D)[c] = o;
+      if (c == 0) *reinterpret_cast<float2*>(a.stats + (piece0 + h) * 2) = make_float2(M, den);
     } else {
-      reinterpret_cast<float4*>(a.acc + row * D)[c] = o;
+      const float inv = den == 0.f ? 0.f : 1.0f / den;
+      const float4 r = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+      // (nothing seen, or logits of -inf alone: zeros)
+      store_out<DT>(a.out, out_row(a, b, g, h), D, c, den == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : r);
+      if (SUMS && c == 0) norm[h] = make_float2(M, inv);
     }
-    if ((SUMS || a.parts > 1) && c == 0) *reinterpret_cast<float2*>(a.stats + row * 2) = make_float2(M, den);
+  }
+  if (dealt) {
+    if (part == 0 && threadIdx.x == 0) a.pieces[pair] = make_int2(blockIdx.x, parts);
+    return;
+  }
+  if constexpr (SUMS) {
+    // the whole walk is here: its logits, which the waves have stored, become weights
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * w.n; i += kWinThreads) add_weight(a, w, pair, i, norm);
   }
 }
 
-// Grid (heads + row groups, Hkv, B): with more than one part, the first T*G
-// work-groups of a KV head join the parts of one query row each; the others (sums)
-// take kFinishRows rows of the walk each.
+// Grid (heads + row groups, Hkv, B): the first T*G work-groups of a KV head join the
+// pieces of one query row each; the others (sums) take kFinishThreads rows of the walk each.
 constexpr int kFinishThreads = 256;
-constexpr int kFinishRows = kFinishThreads;
 
-// (max, 1 / sum) of query row r over the parts, by the 16 lanes that share it
-__device__ __forceinline__ float2 row_norm(const WindowArgs& a, size_t pair, int r, int sub) {
-  const float2* st = reinterpret_cast<const float2*>(a.stats) + (pair * a.T * a.G + r) * a.parts;
+// (max, 1 / sum) of query row r over the pieces, by the 16 lanes that share it
+__device__ __forceinline__ float2 row_norm(const WindowArgs& a, int2 p, int r, int sub) {
+  const int TG = a.T * a.G;
+  const float2* st = reinterpret_cast<const float2*>(a.stats) + static_cast<size_t>(p.x) * TG + r;
   float M = kNoLogit;
-  for (int i = sub; i < a.parts; i += 16) M = fmaxf(M, st[i].x);
+  for (int i = sub; i < p.y; i += 16) M = fmaxf(M, st[static_cast<size_t>(i) * TG].x);
   M = group_max_f32(M, 16);
   float l = 0.f;
-  for (int i = sub; i < a.parts; i += 16) l = fmaf(fast_exp2(st[i].x - M), st[i].y, l);
+  for (int i = sub; i < p.y; i += 16) {
+    const float2 v = st[static_cast<size_t>(i) * TG];
+    l = fmaf(fast_exp2(v.x - M), v.y, l);
+  }
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) l += __shfl_xor(l, o, 16);
   return make_float2(M, l == 0.f ? 0.f : 1.0f / l);
@@ -291,17 +528,25 @@ __global__ __launch_bounds__(kFinishThreads) void finish_kernel(const WindowArgs
   const int TG = a.T * a.G;
   __shared__ float2 norm[16];
   __shared__ float4 part_sum[R][COLS];
-  if (static_cast<int>(blockIdx.x) < heads) {
+  const int2 pieces = a.pieces[pair];
+  const WindowWalk w = walk_of(a, b);
+  const int i0 = (static_cast<int>(blockIdx.x) - heads) * kFinishThreads;
+  if (i0 >= 32 * w.n) return;  // (no rows of the walk left for this work-group)
+  const int2 p = w.n > 0 ? pieces : make_int2(0, 0);  // first piece, number of pieces
+  if (i0 < 0) {
     const int h = blockIdx.x;
-    if (tid < 16) norm[tid] = row_norm(a, pair, h, tid);
+    if (tid < 16) {
+      const float2 mn = row_norm(a, p, h, tid);
+      if (tid == 0) norm[0] = mn;
+    }
     __syncthreads();
     const float2 mn = norm[0];
     const int col = tid % COLS, r = tid / COLS;
-    const size_t row0 = (pair * TG + h) * a.parts;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = r; i < a.parts; i += R) {
-      const float f = fast_exp2(a.stats[(row0 + i) * 2] - mn.x);
-      const float4 x = reinterpret_cast<const float4*>(a.acc + (row0 + i) * D)[col];
+    for (int i = r; i < p.y; i += R) {
+      const size_t row = static_cast<size_t>(p.x + i) * TG + h;
+      const float f = fast_exp2(a.stats[row * 2] - mn.x);
+      const float4 x = reinterpret_cast<const float4*>(a.acc + row * D)[col];
       o.x = fmaf(f, x.x, o.x);
       o.y = fmaf(f, x.y, o.y);
       o.z = fmaf(f, x.z, o.z);
@@ -325,39 +570,27 @@ __global__ __launch_bounds__(kFinishThreads) void finish_kernel(const WindowArgs
     }
     return;
   }
-  const WindowWalk w(clamp_len(a.seq_len[b], a.max_seq_len), a.T, a.window, a.n_sink);
-  const int i0 = (static_cast<int>(blockIdx.x) - heads) * kFinishRows;
-  if (i0 >= 32 * w.n) return;
   if (tid < 16 * TG) {
-    const float2 mn = row_norm(a, pair, tid >> 4, tid & 15);
+    const float2 mn = row_norm(a, p, tid >> 4, tid & 15);
     if ((tid & 15) == 0) norm[tid >> 4] = mn;
   }
   __syncthreads();
-  const int i = i0 + tid;
-  const int k = i >> 5;
-  if (k >= w.n) return;
-  const int j = w.t0(k) + (i & 31);
-  if (j < w.row_begin(k) || j >= w.row_end(k)) return;
-  const float* z = a.zs + (pair * a.tiles * 32 + i) * a.gp;
-  float s = 0.f;
-  for (int h = 0; h < TG; ++h) s = fmaf(fast_exp2(z[h] - norm[h].x), norm[h].y, s);
-  float* dst = a.attn_sum + pair * a.max_seq_len + j;
-  *dst = j >= w.L - a.T ? s : *dst + s;
+  if (i0 + tid < 32 * w.n) add_weight(a, w, pair, i0 + tid, norm);
 }
 
 template <int DT, int D>
 hipError_t launch_dd(const WindowArgs& a, hipStream_t st) {
-  const dim3 grid(a.parts, a.Hkv, a.B);
+  const dim3 grid = a.groups > 0 ? dim3(a.groups) : dim3(1, a.Hkv, a.B);
   const bool paged = a.bs_log2 >= 0, sums = a.attn_sum != nullptr;
   if (paged && sums) hipLaunchKernelGGL((window_kernel<DT, D, true, true>), grid, dim3(kWinThreads), 0, st, a);
   else if (paged) hipLaunchKernelGGL((window_kernel<DT, D, true, false>), grid, dim3(kWinThreads), 0, st, a);
   else if (sums) hipLaunchKernelGGL((window_kernel<DT, D, false, true>), grid, dim3(kWinThreads), 0, st, a);
   else hipLaunchKernelGGL((window_kernel<DT, D, false, false>), grid, dim3(kWinThreads), 0, st, a);
   if (hipError_t e = hipGetLastError()) return e;
-  const int heads = a.parts > 1 ? a.T * a.G : 0;
-  const int rows = sums ? (a.tiles * 32 + kFinishRows - 1) / kFinishRows : 0;
-  if (heads + rows > 0)
-    hipLaunchKernelGGL((finish_kernel<DT, D>), dim3(heads + rows, a.Hkv, a.B), dim3(kFinishThreads), 0, st, a, heads);
+  if (a.groups == 0) return hipSuccess;
+  const int heads = a.T * a.G;
+  const int rows = sums ? (a.tiles * 32 + kFinishThreads - 1) / kFinishThreads : 0;
+  hipLaunchKernelGGL((finish_kernel<DT, D>), dim3(heads + rows, a.Hkv, a.B), dim3(kFinishThreads), 0, st, a, heads);
   return hipGetLastError();
 }
 
@@ -372,16 +605,21 @@ WindowPlan make_window_plan(const vp_shape& s, const vp_window& w, bool sums) {
   p.tiles = static_cast<int>(tiles);
   const int64_t pairs = static_cast<int64_t>(s.batch) * s.n_kv_heads;
   // one resident round of work-groups, a tile per wave at least
-  const int64_t parts = std::min<int64_t>(resident_groups(s.dtype, s.head_dim) / pairs, (tiles + kWinWaves - 1) / kWinWaves);
-  p.parts = static_cast<int>(std::max<int64_t>(1, parts));
+  const bool one_each = tiles <= VP_ONE_GROUP_TILES || pairs >= VP_ONE_GROUP_PAIRS || pairs * tiles > 0x3fffffff;
+  const int64_t round = resident_groups(s.dtype, s.head_dim);
+  const int64_t most = pairs <= round / 2 ? round : 4 * std::max(round, pairs);
+  p.groups = one_each ? 0 : static_cast<int>(std::min(most, pairs * ((tiles + kWinWaves - 1) / kWinWaves)));
   const int rows = static_cast<int>(T) * (s.n_q_heads / s.n_kv_heads);
   p.gp = 1;
   while (p.gp < rows) p.gp *= 2;
+  const size_t pieces = p.groups;
   size_t off = 0;
   p.stats = off;
-  off = align256(off + static_cast<size_t>(pairs) * rows * p.parts * 2 * 4);
+  off = align256(off + pieces * rows * 2 * 4);
   p.acc = off;
-  if (p.parts > 1) off = align256(off + static_cast<size_t>(pairs) * rows * p.parts * s.head_dim * 4);
+  off = align256(off + pieces * rows * s.head_dim * 4);
+  p.pieces = off;
+  if (p.groups > 0) off = align256(off + static_cast<size_t>(pairs) * 2 * 4);
   p.zs = off;
   if (sums) off = align256(off + static_cast<size_t>(pairs) * p.tiles * 32 * p.gp * 4);
   p.total = off;

@@ -112,6 +112,7 @@ def test_sum_workspace_holds_the_logits():
     assert a <= vp.vp_window_workspace_size(_shape(max_seq_len=1 << 27), _window(), True) + 256 <= 2 * a
     with pytest.raises(vp.VPError):
         vp.vp_window_workspace_size(_shape(), w, 2)
+    assert vp.vp_window_workspace_size(_shape(), _window(window=64), False) == 0  # a short walk needs none
 
 
 # ---------------------------------------------------------------------------

@@ -99,6 +99,17 @@ def test_more_pairs_than_work_groups():
     check(q, K, V, lens, 50, 3, "bf16")
 
 
+def test_no_workspace_where_none_is_needed():
+    q, K, V = draw(2, 2, 1, 4, 2, 64, 200, "bf16")
+    c, qd = Caches(K, V, "bf16"), on_device(q, "bf16")
+    shape, w = c.shape(4), vp.vp_window(window=100, n_sink=4, sm_scale=0.0)
+    assert vp.vp_window_workspace_size(shape, w) == 0
+    out = torch.zeros_like(qd)
+    seq_len = i32([200, 90])
+    vp.vp_window_decode_attn(shape, c.layout(seq_len), w, qd, c.K, c.V, None, out, None, 0)
+    assert torch.equal(out, attention(c, qd, [200, 90], 100, 4))
+
+
 def test_logit_scale():
     q, K, V = draw(9, 2, 1, 8, 2, 128, 150, "bf16")
     check(q, K, V, [150, 77], 60, 2, "bf16", scale=0.37)
