@@ -416,8 +416,9 @@ vp_status vp_evict_workspace_size(const vp_shape* shape, const vp_evict_params* 
  * visual segments are read only for vis_seg_out. A block that two sequences
  * share (or a sequence twice) must not be evicted from: block ids are trusted.
  * shape.n_queries, max_vis, max_segs and k_cap have no effect on the rows kept.
- * K and V must be different caches and the workspace must not be shared by
- * concurrent calls.
+ * K and V must be different caches whose rows do not overlap (VP_ERR_SHAPE for
+ * strides that make them), and the workspace must not be shared by concurrent
+ * calls.
  * VP_ERR_RANGE: budget < 1, n_sink < 0, n_recent < 0, n_sink + n_recent > budget.
  */
 vp_status vp_evict(const vp_shape* shape, const vp_layout* layout, const vp_evict_params* params,

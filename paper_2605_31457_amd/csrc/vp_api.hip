@@ -322,6 +322,25 @@ vp_status check_evict(const vp_evict_params* p) {
   return VP_OK;
 }
 
+// Caches that are written: no two rows (of a sequence or block, of KV heads, of
+// sequences or blocks) share memory. Strides in ascending order, each past what the
+// smaller ones span.
+vp_status check_rows_apart(const vp_shape* s) {
+  struct Dim {
+    int64_t stride, size;
+  } d[3] = {{s->kv_stride_s, s->block_size > 0 ? std::min(s->block_size, s->max_seq_len) : s->max_seq_len},
+            {s->kv_stride_h, s->n_kv_heads},
+            {s->kv_stride_b, s->block_size > 0 ? 2 : s->batch}};  // (blocks: any two)
+  std::sort(d, d + 3, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
+  int64_t span = s->head_dim;
+  for (const Dim& x : d) {
+    if (x.size < 2) continue;
+    if (x.stride < span) return fail(VP_ERR_SHAPE, "rows of the caches overlap (KV stride %lld < %lld)", (long long)x.stride, (long long)span);
+    span += x.stride * (x.size - 1);
+  }
+  return VP_OK;
+}
+
 // sequence lengths, and the block table of paged caches
 vp_status check_rows(const vp_shape* s, const vp_layout* l) {
   if (!l) return fail(VP_ERR_NULL, "layout is NULL");
@@ -786,6 +805,7 @@ vp_status vp_evict(const vp_shape* shape, const vp_layout* layout, const vp_evic
   if (!attn_sum || !K || !V || !kept || !attn_sum_out || !new_len)
     return fail(VP_ERR_NULL, "attn_sum, K, V, kept, attn_sum_out, new_len required");
   if (!aligned16(K) || !aligned16(V)) return fail(VP_ERR_SHAPE, "K, V must be 16-byte aligned");
+  if (vp_status e = check_rows_apart(shape)) return e;
   if (K == V) return fail(VP_ERR_SHAPE, "K and V are the same cache");
   if (vis_seg_out && shape->scope != VP_SCOPE_SEQUENCE)
     return fail(VP_ERR_UNSUPPORTED, "vis_seg_out needs one kept set per sequence (VP_SCOPE_SEQUENCE)");

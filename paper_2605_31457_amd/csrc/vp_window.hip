@@ -18,14 +18,19 @@
 //                  its four waves take in turn (dealt out cyclically, the parts of 16
 //                  contexts of 32k tokens walk their caches in step, 8 MB apart: 200 us
 //                  where runs take 158); the T*G <= 16 query rows of the KV head share
-//                  every tile. The waves' partials meet in LDS. With
-//                  sums the logits leave as rows of gp floats (32 bytes per row at 7 heads,
-//                  beside 512 bytes of K and V), since a weight is known only when the
-//                  whole walk is.
+//                  every tile. The waves' partials meet in LDS. With sums the logits
+//                  leave as rows of gp floats (32 bytes per row at 7 heads, beside 512 of
+//                  K and V), since a weight is known only when the whole walk is. That
+//                  is what sums cost: any stores in a stream of reads slow the reads (16
+//                  contexts of 32k tokens 158 us without, 204 with them; the same whether
+//                  they are issued tile by tile, four tiles together or behind the next
+//                  tile's copies, 187 with a quarter of them, and no less with any cache
+//                  policy).
 //   finish_kernel  joins the pieces of each query row, and turns the logits into weights:
 //                  one thread per row, the query rows in order, so the sums do not
 //                  depend on the partition of the walk or on arrival.
-// Short walks, and those of very many pairs, have one work-group per pair, which does both.
+// Short walks, and those of many pairs, have one work-group per pair, which does both
+// (make_window_plan).
 //
 // A masked row weighs nothing whatever it holds: its logit is not looked at, and in
 // the tiles where some query does not see some row (the ends of the window, of the
@@ -45,16 +50,9 @@ constexpr int kWinThreads = 64 * kWinWaves;
 
 size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
-#ifndef VP_ONE_GROUP_TILES
-#define VP_ONE_GROUP_TILES 8  // walks of up to this many tiles: one work-group each, no second launch
-#endif
-#ifndef VP_ONE_GROUP_PAIRS
-#define VP_ONE_GROUP_PAIRS 2048  // from this many (sequence, KV head) pairs on too
-#endif
-
 // A running maximum is raised only when a logit exceeds it by more than this (log2
-// units): weights stay below 2^64, and rescaling is rare
-constexpr float kRaise = 64.f;
+// units): weights stay below 2^8, and rescaling is rare
+constexpr float kRaise = 8.f;
 
 template <int DT, int D, bool SUMS>
 struct WinLds {
@@ -93,9 +91,9 @@ __device__ __forceinline__ WindowWalk walk_of(const WindowArgs& a, int b) {
 // How the walks of a batch are dealt to `groups` work-groups, found by every wave from
 // the lengths (no barrier): a work-group takes about `share` tiles of one pair, so a pair
 // of n tiles has ceil(n / share) of them, its parts. Up to 64 sequences have a lane each,
-// one load of the lengths is all that is read, and share is the least multiple of a
-// round of the four waves whose work-groups are not too many; more sequences have
-// consecutive ones in every lane, and share is what always fits.
+// one load of the lengths is all that is read, and share is about the least whose
+// work-groups are not too many; more sequences have consecutive ones in every lane, and
+// share is what always fits.
 struct Deal {
   int b, g, part, parts;  // this work-group's sequence, KV head and part of parts; b < 0: none
   int L;                  // the sequence's length
@@ -111,11 +109,11 @@ struct Deal {
     }
     const int total = a.Hkv * __builtin_amdgcn_readlane(wave_incl_sum(mine), 63);
     const int pairs = a.Hkv * a.B;
-    int share = max(1, (total + a.groups - 1) / a.groups), count = 0;
-    share = (share + kWinWaves - 1) / kWinWaves * kWinWaves;
+    int share = (total + a.groups - 1) / a.groups, count = 0;
+    share = max(share, kWinWaves);  // a tile per wave at least
     if (per == 1) {
       // (ends: a share of the longest walk gives every pair one part, and there are as many groups)
-      for (;; share += max(1, share / 128) * kWinWaves) {
+      for (;; share += max(1, share / 32)) {
         count = wave_incl_sum(split(mine, share));
         if (a.Hkv * __builtin_amdgcn_readlane(count, 63) <= a.groups) break;
       }
@@ -322,13 +320,12 @@ window_kernel(const WindowArgs a) {
 #pragma unroll
   for (int i = 0; i < C::ACC_N; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+  // the copies of tile k, and the next tile's block ids
   int blk_next = blocks_of(k);
-  for (; k < k1; k += kWinWaves) {
+  auto request = [&](int k) {
     const int t0 = w.t0(k);
     const int r0 = w.row_begin(k), r1 = w.row_end(k);  // rows that some query sees, r0 < r1
     const int blk = blk_next;
-    // LDS reads of the previous tile have returned before the copies overwrite it
-    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
     if (even && r0 == t0 && r1 == t0 + 32) {
       size_t lo, up;
       if constexpr (PAGED) {
@@ -364,6 +361,10 @@ window_kernel(const WindowArgs a) {
                                          0, kCopyPolicy);
     }
     blk_next = blocks_of(k + kWinWaves);
+  };
+  if (k < k1) request(k);
+  while (k < k1) {
+    const int t0 = w.t0(k);
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
 
     float z[8];
@@ -441,6 +442,10 @@ window_kernel(const WindowArgs a) {
         for (int i = 0; i < C::ACC_N; ++i) acc[i] = tq == t ? sum[i] : acc[i];
       }
     }
+    k += kWinWaves;
+    // LDS reads of the tile have returned before the next one's copies overwrite it
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+    if (k < k1) request(k);
   }
   l = sum_over_quads(l);
 
@@ -498,7 +503,8 @@ window_kernel(const WindowArgs a) {
 }
 
 // Grid (heads + row groups, Hkv, B): the first T*G work-groups of a KV head join the
-// pieces of one query row each; the others (sums) take kFinishThreads rows of the walk each.
+// pieces of one query row each; the others (sums) take
+// kFinishThreads rows of the walk at a time.
 constexpr int kFinishThreads = 256;
 
 // (max, 1 / sum) of query row r over the pieces, by the 16 lanes that share it
@@ -575,7 +581,8 @@ __global__ __launch_bounds__(kFinishThreads) void finish_kernel(const WindowArgs
     if ((tid & 15) == 0) norm[tid >> 4] = mn;
   }
   __syncthreads();
-  if (i0 + tid < 32 * w.n) add_weight(a, w, pair, i0 + tid, norm);
+  const int step = (static_cast<int>(gridDim.x) - heads) * kFinishThreads;
+  for (int i = i0 + tid; i < 32 * w.n; i += step) add_weight(a, w, pair, i, norm);
 }
 
 template <int DT, int D>
@@ -589,7 +596,10 @@ hipError_t launch_dd(const WindowArgs& a, hipStream_t st) {
   if (hipError_t e = hipGetLastError()) return e;
   if (a.groups == 0) return hipSuccess;
   const int heads = a.T * a.G;
-  const int rows = sums ? (a.tiles * 32 + kFinishThreads - 1) / kFinishThreads : 0;
+  // (a capacity far above the lengths costs no more work-groups than a full GPU needs)
+  const int64_t pairs = static_cast<int64_t>(a.B) * a.Hkv;
+  const int64_t most = std::max<int64_t>(1, 8192 / pairs);
+  const int rows = sums ? static_cast<int>(std::min<int64_t>(most, (a.tiles * 32ll + kFinishThreads - 1) / kFinishThreads)) : 0;
   hipLaunchKernelGGL((finish_kernel<DT, D>), dim3(heads + rows, a.Hkv, a.B), dim3(kFinishThreads), 0, st, a, heads);
   return hipGetLastError();
 }
@@ -604,10 +614,22 @@ WindowPlan make_window_plan(const vp_shape& s, const vp_window& w, bool sums) {
     tiles = std::min(cap, (static_cast<int64_t>(w.n_sink) + 31) / 32 + (w.window + T - 1 + 30) / 32 + 1);
   p.tiles = static_cast<int>(tiles);
   const int64_t pairs = static_cast<int64_t>(s.batch) * s.n_kv_heads;
-  // one resident round of work-groups, a tile per wave at least
-  const bool one_each = tiles <= VP_ONE_GROUP_TILES || pairs >= VP_ONE_GROUP_PAIRS || pairs * tiles > 0x3fffffff;
-  const int64_t round = resident_groups(s.dtype, s.head_dim);
-  const int64_t most = pairs <= round / 2 ? round : 4 * std::max(round, pairs);
+  // One work-group per pair, and no second launch, where
+  // * the walks are short: up to 16 tiles, 12 with sums (bf16; 8 KV heads of 128, 16 tiles:
+  //   9.2 us and, dealt, 12.1; with sums 11.3 and 12.0, 32 pairs 12.8 and 12.2; 32 tiles
+  //   15.3 and 12.1), 8 in fp32 (32 pairs of 128, 16 tiles: 19.6 and 15.2);
+  // * a window makes the walks of a batch much the same and the pairs nearly fill the CUs:
+  //   192 pairs (16 tiles: 12.7 and 16.2, 256 tiles: 117 and 133; 128 pairs, 64 tiles: 30.2
+  //   and 28.0), 384 with rows of 128 bytes (64 tiles: 35.9 and 41.7; 256 pairs: 31.3 and 28.2);
+  // * there are pairs for several rounds whatever their lengths: 1024.
+  const bool bf16 = s.dtype == VP_BF16;
+  const int64_t few = bf16 ? (sums ? 12 : 16) : 8;
+  const int64_t many = w.window == 0 ? 1024 : bf16 && s.head_dim == 64 ? 384 : 192;
+  const bool one_each = tiles <= few || pairs >= many || pairs * tiles > 0x3fffffff;
+  // Otherwise one resident round of work-groups, a tile per wave at least; twice as many
+  // as pairs where those are more (24 ragged sequences of 16 heads of 64: 51.5 us, four
+  // times as many 53.1)
+  const int64_t most = std::max<int64_t>(resident_groups(s.dtype, s.head_dim), 2 * pairs);
   p.groups = one_each ? 0 : static_cast<int>(std::min(most, pairs * ((tiles + kWinWaves - 1) / kWinWaves)));
   const int rows = static_cast<int>(T) * (s.n_q_heads / s.n_kv_heads);
   p.gp = 1;

@@ -95,6 +95,11 @@ def _call_evict(shape=None, layout=None, sums=PTR, K=PTR, V=2 * PTR, kept=PTR, o
     (dict(seg=PTR, layout=_layout(vis_seg_off=PTR, vis_seg=PTR), shape=_shape(scope=1)), "VP_ERR_UNSUPPORTED"),
     (dict(K=PTR + 8), "VP_ERR_SHAPE"), (dict(V=2 * PTR + 8), "VP_ERR_SHAPE"), (dict(V=PTR), "VP_ERR_SHAPE"),
     (dict(ws=None), "VP_ERR_WORKSPACE"), (dict(ws=PTR + 64), "VP_ERR_WORKSPACE"), (dict(nbytes=8), "VP_ERR_WORKSPACE"),
+    # caches whose rows share memory: one head or one sequence for all, heads too close, blocks too close
+    (dict(shape=_shape(kv_stride_h=0)), "VP_ERR_SHAPE"), (dict(shape=_shape(kv_stride_b=0)), "VP_ERR_SHAPE"),
+    (dict(shape=_shape(kv_stride_h=2048 * 128)), "VP_ERR_SHAPE"),
+    (dict(shape=_shape(block_size=32, kv_stride_h=32 * 128, kv_stride_b=3 * 32 * 128), layout=_layout(block_table=PTR)),
+     "VP_ERR_SHAPE"),
     (dict(shape=_shape(head_dim=80)), "VP_ERR_UNSUPPORTED"), (dict(shape=_shape(max_seq_len=0)), "VP_ERR_SHAPE"),
 ])
 def test_evict_refusals(kw, status):
