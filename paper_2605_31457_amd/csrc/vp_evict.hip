@@ -210,16 +210,16 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(const EvictArg
   const int tid = threadIdx.x;
   const int row = b * a.U + (a.U == 1 ? 0 : g);
   uint32_t* turns = a.turns + (static_cast<size_t>(b) * a.Hkv + g) * a.turn_words;
-  if (tid == 0)
+  if (tid == 0 && static_cast<int>(blockIdx.x) < a.chunks)
     s_turn = static_cast<int>(__hip_atomic_fetch_add(turns, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
   const int n = a.meta[2 * row], L = a.meta[2 * row + 1];
   const int32_t* kept = a.kept + static_cast<size_t>(row) * a.budget;
-  __syncthreads();
-  const int c = s_turn;
-  if (c == a.chunks) {
+  if (static_cast<int>(blockIdx.x) == a.chunks) {
     if (g == 0) move_segments(a, b, kept, n, L, tid);
     return;
   }
+  __syncthreads();
+  const int c = s_turn;
   if (c == 0 && g == 0 && tid == 0) a.new_len[b] = n;
   const int i0 = c * ROWS;
   if (i0 >= n) return;  // (rows past the end are nobody's source)

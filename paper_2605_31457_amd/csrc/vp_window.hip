@@ -541,22 +541,38 @@ __global__ __launch_bounds__(kFinishThreads) void finish_kernel(const WindowArgs
   const int2 p = w.n > 0 ? pieces : make_int2(0, 0);  // first piece, number of pieces
   if (i0 < 0) {
     const int h = blockIdx.x;
+    const int col = tid % COLS, r = tid / COLS;
+    // the first pieces' partials are requested together with all pieces' statistics
+    constexpr int HELD = 4;
+    float4 x[HELD];
+    float mx[HELD];
+#pragma unroll
+    for (int j = 0; j < HELD; ++j) {
+      const int i = r + j * R;
+      const size_t row = static_cast<size_t>(p.x + (i < p.y ? i : 0)) * TG + h;  // past the end: not used
+      x[j] = reinterpret_cast<const float4*>(a.acc + row * D)[col];
+      mx[j] = a.stats[row * 2];
+    }
     if (tid < 16) {
       const float2 mn = row_norm(a, p, h, tid);
       if (tid == 0) norm[0] = mn;
     }
     __syncthreads();
     const float2 mn = norm[0];
-    const int col = tid % COLS, r = tid / COLS;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = r; i < p.y; i += R) {
+    auto add = [&](float m, const float4& v) {
+      const float f = fast_exp2(m - mn.x);
+      o.x = fmaf(f, v.x, o.x);
+      o.y = fmaf(f, v.y, o.y);
+      o.z = fmaf(f, v.z, o.z);
+      o.w = fmaf(f, v.w, o.w);
+    };
+#pragma unroll
+    for (int j = 0; j < HELD; ++j)
+      if (r + j * R < p.y) add(mx[j], x[j]);
+    for (int i = r + HELD * R; i < p.y; i += R) {
       const size_t row = static_cast<size_t>(p.x + i) * TG + h;
-      const float f = fast_exp2(a.stats[row * 2] - mn.x);
-      const float4 x = reinterpret_cast<const float4*>(a.acc + row * D)[col];
-      o.x = fmaf(f, x.x, o.x);
-      o.y = fmaf(f, x.y, o.y);
-      o.z = fmaf(f, x.z, o.z);
-      o.w = fmaf(f, x.w, o.w);
+      add(a.stats[row * 2], reinterpret_cast<const float4*>(a.acc + row * D)[col]);
     }
     part_sum[r][col] = o;
     __syncthreads();
