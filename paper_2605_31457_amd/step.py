@@ -1,4 +1,5 @@
-"""Device buffers for one decode step and the four C-ABI calls in order.
+"""Device buffers for one decode step and the four C-ABI calls in order, and the
+calls of a bounded cache (window attention, eviction) on the same buffers.
 
 Marshalling only: uploads a ``workloads.Workload`` to the GPU (torch
 allocations), fills the ABI structs and calls vp_visual_mass -> vp_budget ->
@@ -110,6 +111,8 @@ class DeviceStep:
         self.k = torch.zeros(R, **i32)
         self.vis_idx = torch.full((R, self.k_cap), -7, **i32)
         self.out = torch.zeros(B * T, Hq, d, dtype=self.q.dtype, device=self.device)
+        self.attn_sum = None      # running attention weights (window_decode_attn)
+        self._bounded_ws = []
         self.ws_bytes = vp.vp_workspace_size(self.shape)
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
 
@@ -133,6 +136,40 @@ class DeviceStep:
         vp.vp_decode_step(self.shape, self.layout, self.params, self.q, self.K, self.V, self.mass_head,
                           self.mass_seq, self.scores, self.k, self.vis_idx, self.out, self.ws, self.ws_bytes,
                           stream, events)
+
+    # decoding on a bounded cache ------------------------------------------
+    def _workspace(self, nbytes):
+        """A workspace of at least nbytes for the calls below. Smaller ones stay
+        alive: a captured graph may hold their addresses."""
+        if not self._bounded_ws or self._bounded_ws[-1].numel() < nbytes:
+            self._bounded_ws.append(torch.empty(nbytes, dtype=torch.uint8, device=self.device))
+        return self._bounded_ws[-1]
+
+    def window_decode_attn(self, window=0, n_sink=0, sums=False, sm_scale=0.0, stream=None):
+        """vp_window_decode_attn into ``out``: the positions before each query that
+        lie in the window (0: all) or are among the first n_sink. With ``sums`` the
+        rows' weights are added to ``attn_sum`` [B, Hkv, S_cap] (zeros at first)."""
+        if sums and self.attn_sum is None:
+            self.attn_sum = torch.zeros(self.w.B, self.w.Hkv, self.w.S_cap, dtype=torch.float32, device=self.device)
+        opt = vp.vp_window(window=window, n_sink=n_sink, sm_scale=sm_scale)
+        nbytes = vp.vp_window_workspace_size(self.shape, opt, sums)
+        vp.vp_window_decode_attn(self.shape, self.layout, opt, self.q, self.K, self.V, self.attn_sum if sums else None,
+                                 self.out, self._workspace(nbytes), nbytes, stream)
+
+    def evict(self, budget, n_sink=0, n_recent=0, stream=None):
+        """vp_evict in place, by ``attn_sum``: K, V, attn_sum and seq_len of every
+        sequence of more than ``budget`` rows, and the visual segments (with one kept
+        set per sequence). Returns the kept positions [B * (1 or Hkv), budget]. With
+        ``kv_groups`` every KV head keeps its own rows, and segments would differ by
+        head: sequences with visual tokens need the method's one set."""
+        if self.attn_sum is None:
+            raise RuntimeError("evict: no attention sums yet (window_decode_attn(sums=True) accumulates them)")
+        opt = vp.vp_evict_params(budget=budget, n_sink=n_sink, n_recent=n_recent)
+        kept = torch.empty(self.w.B * self.rows, budget, dtype=torch.int32, device=self.device)
+        nbytes = vp.vp_evict_workspace_size(self.shape, opt)
+        vp.vp_evict(self.shape, self.layout, opt, self.attn_sum, self.K, self.V, kept, self.attn_sum,
+                    None if self.kv_groups else self.seg, self.seq_len, self._workspace(nbytes), nbytes, stream)
+        return kept
 
     def run(self, fused=True, stream=None):
         self.visual_mass(fused, stream)

@@ -116,6 +116,18 @@ def _stream(s):
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
+def _on_current_device(fn, *args):
+    """Tensors among args lie on the current GPU, on which the call will run."""
+    tensors = [x for x in args if x is not None and not isinstance(x, int)]
+    if not tensors:
+        return
+    import torch
+    here = torch.cuda.current_device()
+    for x in tensors:
+        if x.get_device() != here:
+            raise ValueError(f"{fn}: a tensor is on {x.device}, the current device is cuda:{here}")
+
+
 def _check(fn, status):
     if status != 0:
         raise VPError(fn, status, lib().vp_last_error().decode())
@@ -237,6 +249,7 @@ def vp_window_workspace_size(shape: vp_shape, window: vp_window, with_sums: bool
 def vp_window_decode_attn(shape, layout, window, q, K, V, attn_sum, out, workspace, workspace_bytes=None, stream=None):
     """Attention over a sliding window and the first tokens; attn_sum None, or
     float32 [B, Hkv, max_seq_len] to which the rows' weights are added."""
+    _on_current_device("vp_window_decode_attn", q, K, V, attn_sum, out, workspace)
     nbytes = workspace.numel() * workspace.element_size() if workspace_bytes is None else workspace_bytes
     _check("vp_window_decode_attn", lib().vp_window_decode_attn(
         ctypes.byref(shape), ctypes.byref(layout), ctypes.byref(window), _p(q), _p(K), _p(V), _p(attn_sum), _p(out),
@@ -255,6 +268,7 @@ def vp_evict(shape, layout, params, attn_sum, K, V, kept, attn_sum_out, vis_seg_
     """Keeps the first, the last and the most attended rows of every sequence, in
     place; vis_seg_out may be None. attn_sum_out, vis_seg_out and new_len may be the
     arrays that attn_sum and the layout name."""
+    _on_current_device("vp_evict", attn_sum, K, V, kept, attn_sum_out, vis_seg_out, new_len, workspace)
     nbytes = workspace.numel() * workspace.element_size() if workspace_bytes is None else workspace_bytes
     _check("vp_evict", lib().vp_evict(
         ctypes.byref(shape), ctypes.byref(layout), ctypes.byref(params), _p(attn_sum), _p(K), _p(V), _p(kept),

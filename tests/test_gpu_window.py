@@ -110,6 +110,23 @@ def test_no_workspace_where_none_is_needed():
     assert torch.equal(out, attention(c, qd, [200, 90], 100, 4))
 
 
+def test_tensors_elsewhere_are_refused():
+    q, K, V = draw(2, 1, 1, 4, 2, 64, 50, "bf16")
+    c, qd = Caches(K, V, "bf16"), on_device(q, "bf16")
+    shape, w, seq_len = c.shape(4), vp.vp_window(window=0, n_sink=0, sm_scale=0.0), i32([50])
+    out = torch.zeros_like(qd)
+    for args in ((qd.cpu(), c.K, c.V, None, out), (qd, c.K, c.V.cpu(), None, out), (qd, c.K, c.V, torch.zeros(1, 2, 50), out)):
+        with pytest.raises(ValueError):
+            vp.vp_window_decode_attn(shape, c.layout(seq_len), w, *args, None, 1 << 30)
+    assert float(out.abs().max()) == 0
+    p = vp.vp_evict_params(budget=10, n_sink=0, n_recent=0)
+    s = torch.ones(1, 2, 50, device=DEV)
+    with pytest.raises(ValueError):
+        vp.vp_evict(shape, c.layout(seq_len), p, s, c.K, c.V, torch.zeros(1, 10, dtype=torch.int32), s, None, seq_len,
+                    torch.zeros(4096, dtype=torch.uint8, device=DEV))
+    assert seq_len.tolist() == [50]
+
+
 def test_logit_scale():
     q, K, V = draw(9, 2, 1, 8, 2, 128, 150, "bf16")
     check(q, K, V, [150, 77], 60, 2, "bf16", scale=0.37)
