@@ -197,46 +197,68 @@ struct StoreLogits {
   }
 };
 
-// Row i of the walk (tile i / 32) gets its weights of the T*G query rows, in order:
-// norm holds their (max, 1 / sum)
+// One row of the walk on its way to its weight: row i is row i % 32 of tile i / 32
 template <int GP>
-__device__ __forceinline__ void add_weight_gp(const WindowArgs& a, const WindowWalk& w, size_t pair, int i,
-                                              const float2* norm) {
-  const int k = i >> 5;
-  const int j = w.t0(k) + (i & 31);
-  if (j < w.row_begin(k) || j >= w.row_end(k)) return;
-  float z[GP];
-  const float* src = a.zs + (pair * a.tiles * 32 + i) * GP;
-  if constexpr (GP >= 4) {
+struct RowWeight {
+  float z[GP];  // its logits
+  float old;    // its sum so far
+  float* dst;   // null: no row that a query sees
+  __device__ __forceinline__ RowWeight(const WindowArgs& a, const WindowWalk& w, size_t pair, int i) : dst(nullptr) {
+    const int k = i >> 5;
+    const int j = w.t0(k) + (i & 31);
+    if (k >= w.n || j < w.row_begin(k) || j >= w.row_end(k)) return;
+    const float* src = a.zs + (pair * a.tiles * 32 + i) * GP;
+    if constexpr (GP >= 4) {
 #pragma unroll
-    for (int c = 0; c < GP / 4; ++c) {
-      const float4 v = reinterpret_cast<const float4*>(src)[c];
-      z[4 * c] = v.x;
-      z[4 * c + 1] = v.y;
-      z[4 * c + 2] = v.z;
-      z[4 * c + 3] = v.w;
+      for (int c = 0; c < GP / 4; ++c) {
+        const float4 v = reinterpret_cast<const float4*>(src)[c];
+        z[4 * c] = v.x;
+        z[4 * c + 1] = v.y;
+        z[4 * c + 2] = v.z;
+        z[4 * c + 3] = v.w;
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < GP; ++c) z[c] = src[c];
     }
-  } else {
-#pragma unroll
-    for (int c = 0; c < GP; ++c) z[c] = src[c];
+    dst = a.attn_sum + pair * a.max_seq_len + j;
+    old = j >= w.L - a.T ? 0.f : *dst;
   }
-  float* dst = a.attn_sum + pair * a.max_seq_len + j;
-  const float old = j >= w.L - a.T ? 0.f : *dst;
-  float s = 0.f;
-  const int TG = a.T * a.G;
+  // adds the weights of its r query rows, in order: norm holds their (max, 1 / sum)
+  __device__ __forceinline__ void add(const float2* norm, int r) const {
+    if (!dst) return;
+    float s = 0.f;
 #pragma unroll
-  for (int h = 0; h < GP; ++h)
-    if (h < TG) s = fmaf(fast_exp2(z[h] - norm[h].x), norm[h].y, s);
-  *dst = old + s;
+    for (int h = 0; h < GP; ++h)
+      if (h < r) s = fmaf(fast_exp2(z[h] - norm[h].x), norm[h].y, s);
+    *dst = old + s;
+  }
+};
+
+// Rows i0 + threadIdx.x, + step, ... of the walk get their weights; the first row's
+// logits are requested before `ready` (which ends in a barrier) makes norm.
+template <int GP, typename Ready>
+__device__ __forceinline__ void add_weights_gp(const WindowArgs& a, const WindowWalk& w, size_t pair, int i0, int step,
+                                               const float2* norm, Ready ready) {
+  int i = i0 + static_cast<int>(threadIdx.x);
+  RowWeight<GP> row(a, w, pair, i);
+  ready();
+  for (;;) {
+    row.add(norm, a.T * a.G);
+    i += step;
+    if (i >= 32 * w.n) return;
+    row = RowWeight<GP>(a, w, pair, i);
+  }
 }
-__device__ __forceinline__ void add_weight(const WindowArgs& a, const WindowWalk& w, size_t pair, int i,
-                                           const float2* norm) {
+template <typename Ready>
+__device__ __forceinline__ void add_weights(const WindowArgs& a, const WindowWalk& w, size_t pair, int i0, int step,
+                                            const float2* norm, Ready ready) {
   switch (a.gp) {
-    case 1: add_weight_gp<1>(a, w, pair, i, norm); break;
-    case 2: add_weight_gp<2>(a, w, pair, i, norm); break;
-    case 4: add_weight_gp<4>(a, w, pair, i, norm); break;
-    case 8: add_weight_gp<8>(a, w, pair, i, norm); break;
-    default: add_weight_gp<16>(a, w, pair, i, norm); break;
+    case 1: add_weights_gp<1>(a, w, pair, i0, step, norm, ready); break;
+    case 2: add_weights_gp<2>(a, w, pair, i0, step, norm, ready); break;
+    case 4: add_weights_gp<4>(a, w, pair, i0, step, norm, ready); break;
+    case 8: add_weights_gp<8>(a, w, pair, i0, step, norm, ready); break;
+    default: add_weights_gp<16>(a, w, pair, i0, step, norm, ready); break;
   }
 }
 
@@ -498,7 +520,7 @@ window_kernel(const WindowArgs a) {
     // the whole walk is here: its logits, which the waves have stored, become weights
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
     __syncthreads();
-    for (int i = threadIdx.x; i < 32 * w.n; i += kWinThreads) add_weight(a, w, pair, i, norm);
+    add_weights(a, w, pair, 0, kWinThreads, norm, [] {});
   }
 }
 
@@ -592,13 +614,14 @@ __global__ __launch_bounds__(kFinishThreads) void finish_kernel(const WindowArgs
     }
     return;
   }
-  if (tid < 16 * TG) {
-    const float2 mn = row_norm(a, p, tid >> 4, tid & 15);
-    if ((tid & 15) == 0) norm[tid >> 4] = mn;
-  }
-  __syncthreads();
   const int step = (static_cast<int>(gridDim.x) - heads) * kFinishThreads;
-  for (int i = i0 + tid; i < 32 * w.n; i += step) add_weight(a, w, pair, i, norm);
+  add_weights(a, w, pair, i0, step, norm, [&] {
+    if (tid < 16 * TG) {
+      const float2 mn = row_norm(a, p, tid >> 4, tid & 15);
+      if ((tid & 15) == 0) norm[tid >> 4] = mn;
+    }
+    __syncthreads();
+  });
 }
 
 template <int DT, int D>
