@@ -33,24 +33,15 @@ __device__ __forceinline__ uint32_t sum_key(float f) {
   return f != f ? 0xffffffffu : order_key(f + 0.f);
 }
 
-// score of row j of kept list u of sequence b
-__device__ __forceinline__ float row_score(const EvictArgs& a, int b, int u, int j) {
-  const float* s = a.sum + (static_cast<size_t>(b) * a.Hkv + u) * a.max_seq_len + j;
-  if (a.U == a.Hkv) return *s;
-  double t = 0.0;
-  for (int g = 0; g < a.Hkv; ++g) t += static_cast<double>(s[static_cast<size_t>(g) * a.max_seq_len]);
-  return static_cast<float>(t);
-}
-
-// scores of rows j0, j0 + 64, ... (at most last), the heads outermost: every head's
+// scores of rows j0, j0 + STEP, ... (at most last) of kept list u, the heads outermost: every head's
 // loads are issued together (heads innermost: 40 us for 16 sequences of 12k rows, 4 KV
 // heads, where this takes 17)
-template <int KPT>
+template <int KPT, int STEP = 64>
 __device__ __forceinline__ void row_scores(const EvictArgs& a, int b, int u, int j0, int last, float (&score)[KPT]) {
   const float* s = a.sum + (static_cast<size_t>(b) * a.Hkv + u) * a.max_seq_len;
   if (a.U == a.Hkv) {
 #pragma unroll
-    for (int j = 0; j < KPT; ++j) score[j] = s[min(j0 + 64 * j, last)];
+    for (int j = 0; j < KPT; ++j) score[j] = s[min(j0 + STEP * j, last)];
     return;
   }
   constexpr int N = KPT < 16 ? KPT : 16;  // rows in flight
@@ -63,7 +54,7 @@ __device__ __forceinline__ void row_scores(const EvictArgs& a, int b, int u, int
     for (int g = 0; g < a.Hkv; ++g, sg += a.max_seq_len) {
       float v[N];
 #pragma unroll
-      for (int j = 0; j < N; ++j) v[j] = sg[min(j0 + 64 * (c + j), last)];
+      for (int j = 0; j < N; ++j) v[j] = sg[min(j0 + STEP * (c + j), last)];
 #pragma unroll
       for (int j = 0; j < N; ++j) t[j] += static_cast<double>(v[j]);
     }
@@ -130,11 +121,20 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
     select_from_registers(sh, tab, keys, k, false, kmin, kmax, kept + S, tid, lane, wid);
   } else {
     uint32_t* keys = a.keys + static_cast<size_t>(row) * a.max_seq_len;
-    for (int i = tid; i < n; i += kSelThreads) {
-      const uint32_t x = sum_key(row_score(a, b, u, S + i));
-      keys[i] = x;
-      kmin = min(kmin, x);
-      kmax = max(kmax, x);
+    constexpr int kBatch = 8;  // rows in flight per thread
+    for (int base = 0; base < n; base += kBatch * kSelThreads) {
+      float score[kBatch];
+      row_scores<kBatch, kSelThreads>(a, b, u, S + base + tid, S + n - 1, score);
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int i = base + j * kSelThreads + tid;
+        if (i < n) {
+          const uint32_t x = sum_key(score[j]);
+          keys[i] = x;
+          kmin = min(kmin, x);
+          kmax = max(kmax, x);
+        }
+      }
     }
     __threadfence_block();
     block_key_range(sh, kmin, kmax, lane, wid);  // (its barrier puts the keys before the reads)

@@ -178,6 +178,28 @@ def test_many_sequences(dtype, d, Hkv, groups):
     check(K, V, sums, lens, 400, 4, 64, groups, dtype, page=32)
 
 
+def test_offsets_past_32_bits():
+    """Sequences 6 GB apart: byte and element offsets of the second one pass 2^32."""
+    d, Hkv, cap, stride = 128, 2, 300, 3 << 30
+    K, V, sums = draw(21, 2, Hkv, cap, d)
+    c = Caches.__new__(Caches)
+    c.dtype, c.page, c.cap, c.table = "bf16", 0, cap, None
+    views = []
+    for src in (K, V):
+        x = torch.empty(stride + Hkv * cap * d, dtype=torch.bfloat16, device=DEV)
+        views.append(torch.as_strided(x, (2, Hkv, cap, d), (stride, cap * d, d, 1)))
+        views[-1].copy_(torch.from_numpy(src).to(torch.bfloat16))
+    c.K, c.V = views
+    kept, _, new_len, _ = evict(c, 4, torch.from_numpy(sums).to(DEV), [300, 299], 150, 4, 20, True)
+    got = c.get()
+    for b, L in enumerate((300, 299)):
+        for h in range(Hkv):
+            rows = CO.kept_rows(sums[b, h], L, 150, 4, 20)
+            assert np.array_equal(kept[b, h], rows)
+            for x, src in zip(got, (K, V)):
+                assert np.array_equal(x[b, h, :150], src[b, h, rows]) and np.array_equal(x[b, h, 150:], src[b, h, 150:])
+
+
 def test_evicting_again_and_again():
     """In place, round after round with new rows appended, as a decode loop does."""
     K, V, sums = draw(12, 2, 2, 400)

@@ -56,6 +56,30 @@ def test_windows_and_sinks(dtype, T, Hq, Hkv, d, window, n_sink):
     check(q, K, V, LENS, window, n_sink, dtype)
 
 
+@pytest.mark.parametrize("window,n_sink", [(0, 0), (0, 9), (520, 0), (576, 4), (600, 40), (640, 100), (550, 500),
+                                           (900, 2 ** 31 - 1)])
+@pytest.mark.parametrize("dtype,T,Hq,Hkv,d,page", [("bf16", 1, 4, 2, 128, 0), ("bf16", 3, 5, 1, 64, 16), ("f32", 2, 2, 2, 64, 0)])
+def test_long_walks(dtype, T, Hq, Hkv, d, page, window, n_sink):
+    """Walks of more tiles than one work-group takes, shared out by the lengths: ragged
+    ones, empty sequences first, last and in between; the rows that nobody sees are NaN."""
+    lens = [0, 1000, 1, 33, 0, 0, 519, 520, 521, 577, 640, 777, 992, 0]
+    q, K, V = draw(window + n_sink % 97, len(lens), T, Hq, Hkv, d, 1001, dtype)
+    for b, L in enumerate(lens):
+        if window:
+            K[b, :, min(n_sink, L):max(min(n_sink, L), L - T - window + 1)] = np.nan
+            V[b, :, min(n_sink, L):max(min(n_sink, L), L - T - window + 1)] = np.nan
+    check(q, K, V, lens, window, n_sink, dtype, page=page)
+
+
+@pytest.mark.parametrize("B,Hkv,cap,window", [(65, 2, 700, 0), (130, 1, 700, 600), (300, 1, 620, 0), (500, 2, 560, 0)])
+def test_long_walks_of_many_sequences(B, Hkv, cap, window):
+    """More sequences than a wave has lanes."""
+    q, K, V = draw(B, B, 1, 2 * Hkv, Hkv, 64, cap, "bf16")
+    g = np.random.default_rng(B)
+    lens = np.where(g.random(B) < 0.2, 0, g.integers(1, cap + 1, B)).tolist()
+    check(q, K, V, lens, window, 0, "bf16")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("T,Hq,Hkv", [(1, 1, 1), (1, 16, 1), (2, 6, 3), (3, 10, 2), (16, 2, 2), (4, 8, 2), (1, 5, 5)])
