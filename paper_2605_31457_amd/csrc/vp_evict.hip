@@ -63,6 +63,52 @@ __device__ __forceinline__ void row_scores(const EvictArgs& a, int b, int u, int
   }
 }
 
+// Writes first + rank of the kept ranks (every key > T and the first `need` keys == T) in
+// ascending order to out, from keys in registers; keys of slots past the last rank are 0
+// (no sum has that key). Eviction keeps a good part of its rows, so every slot is a
+// compare, whose mask the lanes count themselves in, and a store of consecutive words.
+// Bound by instruction issue (a SIMD runs four of the block's waves): lanes that walk only
+// their own kept slots, as the sparse selection of vp_blocks.h has them, take 9.7 us for
+// 16k of 32k rows, this 4.5. One barrier.
+template <int KPT>
+__device__ __forceinline__ void dense_compaction(SelectShared& sh, const RegKeys<KPT>& keys, int need, uint32_t T,
+                                                 int32_t* out, int first, int lane, int wid) {
+  int gt = 0, eq = 0;  // of the wave
+#pragma unroll
+  for (int j = 0; j < KPT; ++j) gt += __popcll(__ballot(keys.u[j] > T));
+  if (need > 0) {
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) eq += __popcll(__ballot(keys.u[j] == T));
+  }
+  if (lane == 0) {
+    sh.gt[wid] = gt;
+    sh.eq[wid] = eq;
+  }
+  __syncthreads();
+  gt = __builtin_amdgcn_readfirstlane(waves_below(sh.gt, wid));
+  const int rank0 = first + keys.r0;
+  if (need == 0) {
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) {
+      const bool mine = keys.u[j] > T;
+      const uint64_t mask = __ballot(mine);
+      if (mine) out[gt + lanes_below(mask)] = rank0 + 64 * j;
+      gt += __popcll(mask);
+    }
+    return;
+  }
+  eq = __builtin_amdgcn_readfirstlane(waves_below(sh.eq, wid));
+#pragma unroll
+  for (int j = 0; j < KPT; ++j) {
+    const bool over = keys.u[j] > T, tied = keys.u[j] == T;
+    const uint64_t bgt = __ballot(over), beq = __ballot(tied);
+    const int e = eq + lanes_below(beq);  // equal keys before this lane's
+    if (over || (tied && e < need)) out[gt + lanes_below(bgt) + min(need, e)] = rank0 + 64 * j;
+    gt += __popcll(bgt);
+    eq += __popcll(beq);
+  }
+}
+
 // KPT > 0: the keys in registers (max_seq_len <= KPT * kSelThreads); 0: in the workspace
 template <int KPT>
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictArgs a) {
@@ -95,14 +141,6 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
   for (int i = tid; i < S; i += kSelThreads) kept[i] = i;
   for (int i = tid; i < R; i += kSelThreads) kept[C - R + i] = L - R + i;
   if (k == 0) return;
-  if (tid == 0) {
-    // one segment: candidate r is row S + r
-    tab.st[0] = S;
-    tab.en[0] = S + n;
-    tab.rk[0] = 0;
-    tab.rk[1] = n;
-    tab.n = 1;
-  }
   for (int i = tid; i < kHistWords; i += kSelThreads) sh.hist[i] = 0;
   uint32_t kmin = 0xffffffffu, kmax = 0u;
   if constexpr (KPT > 0) {
@@ -118,7 +156,18 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
       kmax = max(kmax, keys.u[j]);
     }
     block_key_range(sh, kmin, kmax, lane, wid);
-    select_from_registers(sh, tab, keys, k, false, kmin, kmax, kept + S, tid, lane, wid);
+    // slots past n: a key below every other
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) keys.u[j] = keys.rank(j) < n ? keys.u[j] : 0u;
+    int need = k;
+    const uint32_t T = radix_select(
+        sh,
+        [&](auto visit) {
+#pragma unroll
+          for (int j = 0; j < KPT; ++j) visit(keys.u[j]);
+        },
+        need, kmin, kmax, tid, lane, wid);
+    dense_compaction(sh, keys, need, T, kept + S, S, lane, wid);
   } else {
     uint32_t* keys = a.keys + static_cast<size_t>(row) * a.max_seq_len;
     constexpr int kBatch = 8;  // rows in flight per thread
@@ -135,6 +184,14 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
           kmax = max(kmax, x);
         }
       }
+    }
+    if (tid == 0) {
+      // one segment: candidate r is row S + r
+      tab.st[0] = S;
+      tab.en[0] = S + n;
+      tab.rk[0] = 0;
+      tab.rk[1] = n;
+      tab.n = 1;
     }
     __threadfence_block();
     block_key_range(sh, kmin, kmax, lane, wid);  // (its barrier puts the keys before the reads)
