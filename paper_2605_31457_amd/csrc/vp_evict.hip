@@ -10,17 +10,17 @@
 // Two launches:
 //   evict_select_kernel  one 1024-thread work-group per kept list: sort keys of the rows
 //                        in between (registers up to 32768 rows, the workspace beyond),
-//                        radix select and ordered compaction of vp_blocks.h;
-//   evict_move_kernel    the rows, K and V. Bound: HBM, every
-//                        moved row read and written once.
+//                        the radix select of vp_blocks.h, the kept rows in order;
+//   evict_move_kernel    the rows. Bound: HBM, K and V of every moved row read and
+//                        written once.
 // Row i comes from kept[i] >= i, in place: it may be written over once the rows that are
 // read from there have been read, and those have lower indices. A work-group reads all of
 // its rows, says so, waits until the work-groups of lower rows have said so and then
 // writes. The work-groups of a KV head take their rows in the order in which they begin
 // (a counter), so what a work-group waits for has begun and waits for nothing before it
-// reads: every wait ends, in whatever order the GPU starts them. (One work-group per KV
-// head and cache that walks its rows upwards, without waits: 1531 us where this takes
-// 441, 32 x 32k tokens, 4 KV heads of 128, to half.)
+// reads: every wait ends, in whatever order the GPU starts them. 32 x 32k tokens of 4 KV
+// heads of 128 to half: 400 us, 5.3 TB/s read and written (one work-group per KV head and
+// cache that walks its rows upwards, without waits: 1500).
 #include "vp_blocks.h"
 #include "vp_cache.h"
 #include "vp_tile.h"
@@ -33,9 +33,9 @@ __device__ __forceinline__ uint32_t sum_key(float f) {
   return f != f ? 0xffffffffu : order_key(f + 0.f);
 }
 
-// scores of rows j0, j0 + STEP, ... (at most last) of kept list u, the heads outermost: every head's
-// loads are issued together (heads innermost: 40 us for 16 sequences of 12k rows, 4 KV
-// heads, where this takes 17)
+// scores of rows j0, j0 + STEP, ... (at most last) of kept list u, the heads outermost:
+// every head's loads are issued together (heads innermost: the selection of 16 sequences
+// of 12k rows, 4 KV heads, 40 us instead of 17)
 template <int KPT, int STEP = 64>
 __device__ __forceinline__ void row_scores(const EvictArgs& a, int b, int u, int j0, int last, float (&score)[KPT]) {
   const float* s = a.sum + (static_cast<size_t>(b) * a.Hkv + u) * a.max_seq_len;
@@ -207,8 +207,9 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
 }
 
 constexpr int kMoveThreads = 256;
-// Rows per work-group: 128 KB of K and V (32 x 32k tokens: 64 rows of 256 bytes 627 us, 128 494,
-// 256 441), 32 KB where that would leave CUs idle (1 x 8k tokens: 18.1 us, 256 rows 19.7)
+// Rows per work-group: 128 KB of K and V (32 x 32k tokens: 64 rows of 256 bytes 627 us per
+// call, 128 494, 256 441), 32 KB where that would leave CUs idle (1 x 8k tokens: 18.1 us,
+// with 256 rows 19.7)
 constexpr int large_rows(int row_bytes) { return row_bytes > 256 ? 128 : 256; }
 constexpr int small_rows(int row_bytes) { return row_bytes > 256 ? 32 : 64; }
 
@@ -222,8 +223,8 @@ __device__ __forceinline__ void await_word(const uint32_t* p) {
     __builtin_amdgcn_s_sleep(1);
 }
 
-// 16 bytes of a row that moves: its old place is not read again (cached: 513 us where
-// this takes 494, 32 x 32k tokens at 128 rows per work-group)
+// 16 bytes of a row that moves: its old place is not read again (cached: 513 us,
+// read past the caches 494, 32 x 32k tokens at 128 rows per work-group)
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ uint4 load_row(const char* p) {
   const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
@@ -258,7 +259,7 @@ template <int ROWB, int ROWS>
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(const EvictArgs a) {
   constexpr int PIECES = ROWB / 16;
   constexpr int RPR = kMoveThreads / PIECES;  // rows per round of loads
-  constexpr int U = ROWS / RPR;          // rounds
+  constexpr int U = ROWS / RPR;               // rounds
   static_assert(U * RPR == ROWS && ROWS <= kMoveThreads, "rows of a work-group");
   __shared__ int s_turn;
   __shared__ int s_src[ROWS];  // position each row comes from (its own: it stays; -1: no row)

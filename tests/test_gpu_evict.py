@@ -171,6 +171,18 @@ def test_segments_outside_the_sequence_are_clipped():
                             [count(0, 200), count(200, 250)], [count(0, 250), 0]]
 
 
+def test_lengths_outside_the_capacity_are_clipped():
+    K, V, sums = draw(8, 2, 2, 150)
+    dev = torch.from_numpy(sums).to(DEV)
+    runs = []
+    for lens in ([900, -7], [150, 0]):
+        c = Caches(K, V, "bf16")
+        runs.append(evict(c, 2, dev, lens, 64, 2, 9, True) + tuple(c.get()))
+    for x, y in zip(*runs):
+        assert x is None and y is None or np.array_equal(x, y)
+    assert runs[0][2].tolist() == [64, 0]
+
+
 @pytest.mark.parametrize("dtype,d,Hkv,groups", [("bf16", 128, 4, True), ("f32", 128, 2, False), ("bf16", 64, 8, False)])
 def test_many_sequences(dtype, d, Hkv, groups):
     K, V, sums = draw(11, 24, Hkv, 900, d, dtype)
