@@ -17,7 +17,7 @@ struct WindowPlan {
   size_t stats;  // float [groups][T*G][2]          (max, sum) of each work-group's part of a walk
   size_t acc;    // float [groups][T*G][d]          its value partials
   size_t pieces; // int32 [B*Hkv][2]                where a pair's pieces begin, and how many there are
-  size_t zs;     // float [B][Hkv][tiles * 32][gp]  logits (log2 domain) by row of the walk
+  size_t zs;     // float [B][Hkv][tiles * 32][gp]  products q.K by row of the walk
   size_t total;
 };
 WindowPlan make_window_plan(const vp_shape& s, const vp_window& w, bool sums);

@@ -166,6 +166,28 @@ struct Deal {
   }
 };
 
+// Scores of half a tile. fp32: four sums of a quarter of the products each, added in
+// pairs; as one chain of d / 4 matrix instructions the logits, and with them the outputs,
+// are up to twice as far from 64 bits as those of a blocked product.
+template <int DT, int D>
+__device__ __forceinline__ f32x4 score_rows(const unsigned char* kb, int hf, const QFrag<DT, D>& q, int a4, int n16) {
+  if constexpr (DT == VP_BF16) {
+    return score_half<DT, D>(kb, hf, q, a4, n16);
+  } else {
+    using C = Cfg<DT, D>;
+    f32x4 c[4] = {};
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      const float4 k = *reinterpret_cast<const float4*>(kb + C::at(16 * hf + n16, (D / 16) * a4 + s));
+      c[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.x, q.v[4 * s + 0], c[0], 0, 0, 0);
+      c[1] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.y, q.v[4 * s + 1], c[1], 0, 0, 0);
+      c[2] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.z, q.v[4 * s + 2], c[2], 0, 0, 0);
+      c[3] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.w, q.v[4 * s + 3], c[3], 0, 0, 0);
+    }
+    return (c[0] + c[1]) + (c[2] + c[3]);
+  }
+}
+
 // 32 rows at equal steps into an LDS block: those of the tile's lower half from `lower`,
 // the upper half's (TWO; else the same address) from `upper`, both as seen from row 0;
 // row_step holds the lane's offsets of the copies after which they repeat
@@ -200,7 +222,7 @@ struct StoreLogits {
 // One row of the walk on its way to its weight: row i is row i % 32 of tile i / 32
 template <int GP>
 struct RowWeight {
-  float z[GP];  // its logits
+  float z[GP];  // its products q.K
   float old;    // its sum so far
   float* dst;   // null: no row that a query sees
   __device__ __forceinline__ RowWeight(const WindowArgs& a, const WindowWalk& w, size_t pair, int i) : dst(nullptr) {
@@ -225,12 +247,12 @@ struct RowWeight {
     old = j >= w.L - a.T ? 0.f : *dst;
   }
   // adds the weights of its r query rows, in order: norm holds their (max, 1 / sum)
-  __device__ __forceinline__ void add(const float2* norm, int r) const {
+  __device__ __forceinline__ void add(const float2* norm, int r, float zscale) const {
     if (!dst) return;
     float s = 0.f;
 #pragma unroll
     for (int h = 0; h < GP; ++h)
-      if (h < r) s = fmaf(fast_exp2(z[h] - norm[h].x), norm[h].y, s);
+      if (h < r) s = fmaf(fast_exp2(fmaf(z[h], zscale, -norm[h].x)), norm[h].y, s);
     *dst = old + s;
   }
 };
@@ -244,7 +266,7 @@ __device__ __forceinline__ void add_weights_gp(const WindowArgs& a, const Window
   RowWeight<GP> row(a, w, pair, i);
   ready();
   for (;;) {
-    row.add(norm, a.T * a.G);
+    row.add(norm, a.T * a.G, a.zscale);
     i += step;
     if (i >= 32 * w.n) return;
     row = RowWeight<GP>(a, w, pair, i);
@@ -389,12 +411,13 @@ window_kernel(const WindowArgs a) {
     const int t0 = w.t0(k);
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
 
+    // the products q.K unscaled: a weight is 2^(z * zscale - m), one fma and one exponential
     float z[8];
     {
-      const f32x4 c0 = score_half<DT, D>(lds, 0, qf, a4, n16);
-      const f32x4 c1 = score_half<DT, D>(lds, 1, qf, a4, n16);
+      const f32x4 c0 = score_rows<DT, D>(lds, 0, qf, a4, n16);
+      const f32x4 c1 = score_rows<DT, D>(lds, 1, qf, a4, n16);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) z[i] = (i < 4 ? c0[i & 3] : c1[i & 3]) * a.zscale;
+      for (int i = 0; i < 8; ++i) z[i] = i < 4 ? c0[i & 3] : c1[i & 3];
     }
     // value i of this lane is row t0 + pv_token(a4, i). Does every query see every row?
     const int last0 = w.L - a.T;                                     // the first query's own position
@@ -409,7 +432,7 @@ window_kernel(const WindowArgs a) {
       }
     }
     if constexpr (SUMS) {
-      // the tile's logits as 32 rows of gp floats, -inf where a query does not see the row
+      // the tile's products as 32 rows of gp floats, -inf where a query does not see the row
       const int gp = a.gp;
       if (n16 < gp) {
 #pragma unroll
@@ -421,6 +444,7 @@ window_kernel(const WindowArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if ((seen >> i) & 1u) lmax = fmaxf(lmax, z[i]);
+    lmax *= a.zscale;  // (positive)
     if (__builtin_amdgcn_ballot_w64(lmax > m + kRaise)) {
       // the four lanes of a query row share the reference (their weights meet in one MFMA)
       const float tm = max_over_quads(lmax);
@@ -434,7 +458,7 @@ window_kernel(const WindowArgs a) {
     float p[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      p[i] = (seen >> i) & 1u ? fast_exp2(z[i] - m) : 0.f;
+      p[i] = (seen >> i) & 1u ? fast_exp2(fmaf(z[i], a.zscale, -m)) : 0.f;
       l += p[i];
     }
     const unsigned char* vb = lds + C::SUB_ROWS_BYTES;
