@@ -774,6 +774,9 @@ vp_status vp_window_decode_attn(const vp_shape* shape, const vp_layout* layout, 
   a.n_sink = window->n_sink;
   const float sm = window->sm_scale > 0.f ? window->sm_scale : 1.0f / std::sqrt(static_cast<float>(shape->head_dim));
   a.zscale = sm * 1.4426950408889634f;  // log2(e)
+  // weights stay below 2^8, and rescaling is rare; small beside the maximum that precedes
+  // the first row (-FLT_MAX), which every product exceeds
+  a.raise = std::min(8.f / a.zscale, 0x1p100f);
   a.tiles = plan.tiles;
   a.groups = plan.groups;
   a.gp = plan.gp;

@@ -36,6 +36,7 @@ struct WindowArgs {
   int B, Hq, Hkv, G, T, max_seq_len;
   int window, n_sink;
   float zscale;                // sm_scale * log2(e)
+  float raise;                 // a running maximum is raised when a product exceeds it by more
   int tiles, groups, gp;
   float* stats;
   float* acc;

@@ -2,7 +2,7 @@
 // (vp_window_decode_attn), optionally adding every row's attention weight to a
 // running sum.
 //
-//   z_j = sm_scale <q_h, K_j>,  A_j = 2^(z_j - M) / l over the rows j that query t sees,
+//   z_j = <q_h, K_j>,  A_j = 2^(c (z_j - M)) / l over the rows j that query t sees, c = sm_scale log2(e),
 //   out = sum_j A_j V_j,        attn_sum_j += sum over the KV head's query rows of A_j
 //
 // Bound: the K and V rows that any query sees, read once from HBM (the sums add 8 bytes
@@ -50,9 +50,10 @@ constexpr int kWinThreads = 64 * kWinWaves;
 
 size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
-// A running maximum is raised only when a logit exceeds it by more than this (log2
-// units): weights stay below 2^8, and rescaling is rare
-constexpr float kRaise = 8.f;
+// 2^(c (z - m)) of products z and m, m at most a.raise below z: the difference first, so
+// that the weight of the largest product is what it should be however large it is (in one
+// fma, with m scaled and rounded, it is off by 2^(c m 2^-25): from 2^31 on out of range)
+__device__ __forceinline__ float weight_of(const WindowArgs& a, float z, float m) { return fast_exp2((z - m) * a.zscale); }
 
 template <int DT, int D, bool SUMS>
 struct WinLds {
@@ -246,13 +247,13 @@ struct RowWeight {
     dst = a.attn_sum + pair * a.max_seq_len + j;
     old = j >= w.L - a.T ? 0.f : *dst;
   }
-  // adds the weights of its r query rows, in order: norm holds their (max, 1 / sum)
-  __device__ __forceinline__ void add(const float2* norm, int r, float zscale) const {
+  // adds the weights of the query rows, in order: norm holds their (max, 1 / sum)
+  __device__ __forceinline__ void add(const WindowArgs& a, const float2* norm) const {
     if (!dst) return;
     float s = 0.f;
 #pragma unroll
     for (int h = 0; h < GP; ++h)
-      if (h < r) s = fmaf(fast_exp2(fmaf(z[h], zscale, -norm[h].x)), norm[h].y, s);
+      if (h < a.T * a.G) s = fmaf(weight_of(a, z[h], norm[h].x), norm[h].y, s);
     *dst = old + s;
   }
 };
@@ -266,7 +267,7 @@ __device__ __forceinline__ void add_weights_gp(const WindowArgs& a, const Window
   RowWeight<GP> row(a, w, pair, i);
   ready();
   for (;;) {
-    row.add(norm, a.T * a.G, a.zscale);
+    row.add(a, norm);
     i += step;
     if (i >= 32 * w.n) return;
     row = RowWeight<GP>(a, w, pair, i);
@@ -411,7 +412,7 @@ window_kernel(const WindowArgs a) {
     const int t0 = w.t0(k);
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
 
-    // the products q.K unscaled: a weight is 2^(z * zscale - m), one fma and one exponential
+    // the products q.K, unscaled
     float z[8];
     {
       const f32x4 c0 = score_rows<DT, D>(lds, 0, qf, a4, n16);
@@ -444,12 +445,11 @@ window_kernel(const WindowArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if ((seen >> i) & 1u) lmax = fmaxf(lmax, z[i]);
-    lmax *= a.zscale;  // (positive)
-    if (__builtin_amdgcn_ballot_w64(lmax > m + kRaise)) {
+    if (__builtin_amdgcn_ballot_w64(lmax > m + a.raise)) {
       // the four lanes of a query row share the reference (their weights meet in one MFMA)
       const float tm = max_over_quads(lmax);
-      const bool up = tm > m + kRaise;
-      const float al = up ? fast_exp2(m - tm) : 1.f;
+      const bool up = tm > m + a.raise;
+      const float al = up ? weight_of(a, m, tm) : 1.f;
       l *= al;
 #pragma unroll
       for (int i = 0; i < C::ACC_N; ++i) acc[i] *= al;
@@ -458,7 +458,7 @@ window_kernel(const WindowArgs a) {
     float p[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      p[i] = (seen >> i) & 1u ? fast_exp2(fmaf(z[i], a.zscale, -m)) : 0.f;
+      p[i] = (seen >> i) & 1u ? weight_of(a, z[i], m) : 0.f;
       l += p[i];
     }
     const unsigned char* vb = lds + C::SUB_ROWS_BYTES;
@@ -517,7 +517,7 @@ window_kernel(const WindowArgs a) {
     float den = 0.f;
 #pragma unroll
     for (int v = 0; v < kWinWaves; ++v) {
-      const float f = fast_exp2(ws.m[v][h] - M);
+      const float f = weight_of(a, ws.m[v][h], M);
       const float4 x = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(lds_block + v * Q::BYTES) + h * PITCH)[c];
       den = fmaf(f, ws.l[v][h], den);
       o.x = fmaf(f, x.x, o.x);
@@ -563,7 +563,7 @@ __device__ __forceinline__ float2 row_norm(const WindowArgs& a, int2 p, int r, i
   float l = 0.f;
   for (int i = sub; i < p.y; i += 16) {
     const float2 v = st[static_cast<size_t>(i) * TG];
-    l = fmaf(fast_exp2(v.x - M), v.y, l);
+    l = fmaf(weight_of(a, v.x, M), v.y, l);
   }
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) l += __shfl_xor(l, o, 16);
@@ -607,7 +607,7 @@ __global__ __launch_bounds__(kFinishThreads) void finish_kernel(const WindowArgs
     const float2 mn = norm[0];
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     auto add = [&](float m, const float4& v) {
-      const float f = fast_exp2(m - mn.x);
+      const float f = weight_of(a, m, mn.x);
       o.x = fmaf(f, v.x, o.x);
       o.y = fmaf(f, v.y, o.y);
       o.z = fmaf(f, v.z, o.z);

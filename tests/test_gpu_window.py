@@ -231,6 +231,36 @@ def test_large_logits(dtype, page):
     check(q, K, V, [400, 333], 90, 2, dtype, page=page)
 
 
+@pytest.mark.parametrize("dtype,page", [("bf16", 0), ("f32", 0), ("f32", 16)])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("power", [9, 12, 20, 30])
+def test_logits_whose_rounding_exceeds_the_softmax(dtype, page, sign, power):
+    """Logits of up to 10^power, exact in fp32, the largest an eighth of that above the
+    others: its row weighs 1 to the last bit and the others nothing, in walks of one part
+    and of many."""
+    for L in (300, 3001):
+        q = np.zeros((1, 1, 4, 64))
+        q[..., 0] = 1.0
+        g = np.random.default_rng(power)
+        K = np.zeros((1, 2, L, 64))
+        K[0, :, :, 0] = sign * 10.0 ** power * g.uniform(0.25, 0.75, (2, L))
+        best = g.integers(0, L, 2)
+        for h in range(2):
+            K[0, h, best[h], 0] = sign * 10.0 ** power * (0.875 if sign > 0 else 0.125)
+        K = rounded(K, dtype)
+        V = rounded(g.standard_normal((1, 2, L, 64)), dtype)
+        s = torch.ones(1, 2, L, device=DEV)
+        for sums in (None, s):
+            out = attention(Caches(K, V, dtype, page=page), on_device(q, dtype), [L], 0, 0, sums, 1.0)
+            out = out[0, 0].double().cpu().numpy()
+            for h in range(4):
+                assert np.array_equal(out[h], V[0, h // 2, best[h // 2]]), (L, h)
+        want = np.ones((2, L))
+        want[:, L - 1] = 0.0  # (the query's own row is new)
+        want[[0, 1], best] += 2.0
+        assert np.array_equal(s[0].double().cpu().numpy(), want)
+
+
 def test_same_bits_every_time():
     q, K, V = draw(3, 4, 2, 28, 4, 128, 2100, "bf16")
     c = Caches(K, V, "bf16")
