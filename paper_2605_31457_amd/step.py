@@ -8,6 +8,7 @@ libvisionpulse.so.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 
 import numpy as np
@@ -138,6 +139,15 @@ class DeviceStep:
                           stream, events)
 
     # decoding on a bounded cache ------------------------------------------
+    def _order_of(self, stream):
+        """Tensors made in this context are filled, and reused once freed, in the order
+        of the stream that the call runs on."""
+        if stream is None:
+            return contextlib.nullcontext()
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, self.device) if stream else torch.cuda.default_stream(self.device)
+        return torch.cuda.stream(stream)
+
     def _workspace(self, nbytes):
         """A workspace of at least nbytes for the calls below. Smaller ones stay
         alive: a captured graph may hold their addresses."""
@@ -148,13 +158,20 @@ class DeviceStep:
     def window_decode_attn(self, window=0, n_sink=0, sums=False, sm_scale=0.0, stream=None):
         """vp_window_decode_attn into ``out``: the positions before each query that
         lie in the window (0: all) or are among the first n_sink. With ``sums`` the
-        rows' weights are added to ``attn_sum`` [B, Hkv, S_cap] (zeros at first)."""
-        if sums and self.attn_sum is None:
-            self.attn_sum = torch.zeros(self.w.B, self.w.Hkv, self.w.S_cap, dtype=torch.float32, device=self.device)
+        rows' weights are added to ``attn_sum`` [B, Hkv, S_cap] (zeros at first; the first
+        such call makes it, and is not one that a graph captures). Calls of one
+        DeviceStep share its buffers: those on different streams, and replays of graphs
+        of them, have to be ordered by the caller."""
         opt = vp.vp_window(window=window, n_sink=n_sink, sm_scale=sm_scale)
         nbytes = vp.vp_window_workspace_size(self.shape, opt, sums)
+        with self._order_of(stream):
+            if sums and self.attn_sum is None:
+                if torch.cuda.is_current_stream_capturing():  # (every replay would clear it)
+                    raise RuntimeError("window_decode_attn: run it once with sums before capturing it")
+                self.attn_sum = torch.zeros(self.w.B, self.w.Hkv, self.w.S_cap, dtype=torch.float32, device=self.device)
+            ws = self._workspace(nbytes)
         vp.vp_window_decode_attn(self.shape, self.layout, opt, self.q, self.K, self.V, self.attn_sum if sums else None,
-                                 self.out, self._workspace(nbytes), nbytes, stream)
+                                 self.out, ws, nbytes, stream)
 
     def evict(self, budget, n_sink=0, n_recent=0, stream=None):
         """vp_evict in place, by ``attn_sum``: K, V, attn_sum and seq_len of every
@@ -165,10 +182,12 @@ class DeviceStep:
         if self.attn_sum is None:
             raise RuntimeError("evict: no attention sums yet (window_decode_attn(sums=True) accumulates them)")
         opt = vp.vp_evict_params(budget=budget, n_sink=n_sink, n_recent=n_recent)
-        kept = torch.empty(self.w.B * self.rows, budget, dtype=torch.int32, device=self.device)
         nbytes = vp.vp_evict_workspace_size(self.shape, opt)
+        with self._order_of(stream):
+            kept = torch.empty(self.w.B * self.rows, budget, dtype=torch.int32, device=self.device)
+            ws = self._workspace(nbytes)
         vp.vp_evict(self.shape, self.layout, opt, self.attn_sum, self.K, self.V, kept, self.attn_sum,
-                    None if self.kv_groups else self.seg, self.seq_len, self._workspace(nbytes), nbytes, stream)
+                    None if self.kv_groups else self.seg, self.seq_len, ws, nbytes, stream)
         return kept
 
     def run(self, fused=True, stream=None):

@@ -145,3 +145,16 @@ def test_reference_eviction():
     assert CO.kept_rows([0, math.nan, 7, math.inf, 0], 5, 2, 0, 0).tolist() == [1, 3]
     assert CO.kept_rows([3, 2], 2, 4, 1, 1).tolist() == [0, 1]
     assert CO.compact_segments([(0, 2), (2, 2), (4, 2)], [0, 2, 3, 5]) == [(0, 1), (1, 2), (3, 1)]
+
+
+def test_sums_are_not_made_in_a_capture(monkeypatch):
+    """A graph that made the sums would clear them in every replay."""
+    import torch
+
+    from _parity import small_workload
+    from paper_2605_31457_amd import step
+    ds = step.DeviceStep(small_workload(5, 1, 4, 1, 64, [50], [[]]), device="cpu")
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    with pytest.raises(RuntimeError, match="before capturing"):
+        ds.window_decode_attn(0, 4, sums=True)
+    assert ds.attn_sum is None

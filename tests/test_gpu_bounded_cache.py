@@ -164,3 +164,26 @@ def test_evict_needs_sums():
     ds = S.DeviceStep(small_workload(5, 1, 4, 1, 64, [50], [[]]))
     with pytest.raises(RuntimeError):
         ds.evict(10)
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_buffers_made_on_the_calls_own_stream(handle):
+    """The first call on a side stream while the current stream is busy: attn_sum is
+    cleared before the call adds to it, and the rows kept are not given away while
+    the call runs."""
+    w = small_workload(5, 2, 8, 2, 64, [200, 170], [[(5, 60)], [(9, 40)]], S_cap=256)
+    runs = []
+    for side in (None, torch.cuda.Stream()):
+        ds = S.DeviceStep(w)
+        busy = torch.zeros(1 << 28, dtype=torch.float32, device=ds.device)
+        torch.cuda.synchronize()
+        stream = side.cuda_stream if handle and side is not None else side
+        for _ in range(20 if side is not None else 0):
+            busy.add_(1.0)  # (0.5 ms each, on the current stream)
+        ds.window_decode_attn(0, 4, sums=True, stream=stream)
+        kept = ds.evict(128, 4, 32, stream=stream)
+        torch.cuda.synchronize()
+        runs.append([kept, ds.attn_sum, ds.out, ds.K, ds.seq_len])
+    for x, y in zip(*runs):
+        assert torch.equal(x, y)
+    assert float(runs[1][1].sum()) > 0
