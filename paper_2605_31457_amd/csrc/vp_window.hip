@@ -17,12 +17,16 @@
 //                  from the lengths (Deal). A part is a run of consecutive tiles, which
 //                  its four waves take in turn (dealt out cyclically, the parts of 16
 //                  contexts of 32k tokens walk their caches in step, 8 MB apart: 200 us
-//                  where runs take 158); the T*G <= 16 query rows of the KV head share
-//                  every tile. The waves' partials meet in LDS. With sums the logits
+//                  where runs take 157); the T*G <= 16 query rows of the KV head share
+//                  every tile. A wave asks for a tile's K as soon as the products of the
+//                  one before are done and for its V when that one's values are in: asked
+//                  for together, after the values, fp32 rows wait for the matrix
+//                  instructions (8 paged caches of 4k to 9k tokens with sums 69 us, now 60;
+//                  4 of 32 heads 57, now 51; bf16, 64 windows of 8k 161, now 159). The waves' partials meet in LDS. With sums the logits
 //                  leave as rows of gp floats (32 bytes per row at 7 heads, beside 512 of
 //                  K and V), since a weight is known only when the whole walk is. That
 //                  is what sums cost: any stores in a stream of reads slow the reads (16
-//                  contexts of 32k tokens 158 us without, 204 with them; the same whether
+//                  contexts of 32k tokens 157 us without, 204 with them; the same whether
 //                  they are issued tile by tile, four tiles together or behind the next
 //                  tile's copies, 187 with a quarter of them, and no less with any cache
 //                  policy).
@@ -37,6 +41,7 @@
 // sinks and of the sequence) each query's value product has the rows it does not see
 // replaced by zeros, so that a NaN or infinity there stays out of its output.
 #include <algorithm>
+#include <type_traits>
 
 #include "vp_blocks.h"
 #include "vp_cache.h"
@@ -48,6 +53,9 @@ namespace {
 constexpr int kWinWaves = 4;
 constexpr int kWinThreads = 64 * kWinWaves;
 
+// s_waitcnt operand: at most n vector memory operations left (n < 64), others unconstrained
+constexpr int wait_vm(int n) { return kWaitVm0 | (n & 15) | (n >> 4) << 14; }
+
 size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 // 2^(c (z - m)) of products z and m, m at most a.raise below z: the difference first, so
@@ -58,8 +66,11 @@ __device__ __forceinline__ float weight_of(const WindowArgs& a, float z, float m
 template <int DT, int D, bool SUMS>
 struct WinLds {
   using C = Cfg<DT, D>;
-  static constexpr int STAGE = SUMS ? C::STAGE_BYTES : 0;
-  static constexpr int BYTES = 2 * C::SUB_ROWS_BYTES + STAGE;  // per wave: a K block, a V block, a logit stage
+  // per wave: a K block (after the walk its accumulator rows), a V block, a logit stage
+  static constexpr int PITCH = D + 4;  // accumulator rows start on different banks
+  static constexpr int K_BYTES = C::SUB_ROWS_BYTES > 16 * PITCH * 4 ? C::SUB_ROWS_BYTES : 16 * PITCH * 4;
+  static constexpr int V_BYTES = C::SUB_ROWS_BYTES;
+  static constexpr int STAGE_BYTES = SUMS ? C::STAGE_BYTES : 16;
 };
 
 // (max, sum) of the query rows, per wave
@@ -290,7 +301,10 @@ __global__ __launch_bounds__(kWinThreads) __attribute__((amdgpu_waves_per_eu(DT 
 window_kernel(const WindowArgs a) {
   using C = Cfg<DT, D>;
   using Q = WinLds<DT, D, SUMS>;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds_block[kWinWaves * Q::BYTES];
+  // (three arrays: in one, the compiler would have reads of V wait for the copies into K)
+  __shared__ __attribute__((aligned(1024))) unsigned char lds_k[kWinWaves * Q::K_BYTES];
+  __shared__ __attribute__((aligned(1024))) unsigned char lds_v[kWinWaves * Q::V_BYTES];
+  __shared__ __attribute__((aligned(1024))) unsigned char lds_stage[kWinWaves * Q::STAGE_BYTES];
   __shared__ WinStats ws;
   __shared__ float2 norm[16];
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
@@ -298,9 +312,9 @@ window_kernel(const WindowArgs a) {
   const int n16 = lane & 15;
   const int a4 = lane >> 4;
   const int TG = a.T * a.G;
-  unsigned char* lds = lds_block + wave * Q::BYTES;
-  lds_byte* dma = (lds_byte*)lds;
-  float* stage = reinterpret_cast<float*>(lds + 2 * C::SUB_ROWS_BYTES);
+  const unsigned char* kb = lds_k + wave * Q::K_BYTES;
+  const unsigned char* vb = lds_v + wave * Q::V_BYTES;
+  float* stage = reinterpret_cast<float*>(lds_stage + wave * Q::STAGE_BYTES);
   const bool hv = n16 < TG;
   const int tq = hv ? n16 / a.G : 0;
 
@@ -351,7 +365,7 @@ window_kernel(const WindowArgs a) {
   // this part's tiles, and this wave's first one
   int k = static_cast<int>(static_cast<int64_t>(part) * w.n / parts) + wave;
   const int k1 = static_cast<int>(static_cast<int64_t>(part + 1) * w.n / parts);
-  // paged caches: lane r < 32 holds the block of row r, loaded a tile ahead
+  // paged caches: lane r < 32 holds the block of row r, loaded two tiles ahead
   auto blocks_of = [&](int k) -> int {
     int blk = 0;
     if constexpr (PAGED) {
@@ -365,12 +379,13 @@ window_kernel(const WindowArgs a) {
 #pragma unroll
   for (int i = 0; i < C::ACC_N; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  // the copies of tile k, and the next tile's block ids
-  int blk_next = blocks_of(k);
-  auto request = [&](int k) {
+  // the copies of tile k of K, of V or of both
+  lds_byte* const k_block = (lds_byte*)(lds_k + wave * Q::K_BYTES);
+  lds_byte* const v_block = (lds_byte*)(lds_v + wave * Q::V_BYTES);
+  int blk = blocks_of(k), blk_next = 0;  // of the tile that is requested, and of the next one
+  auto request = [&](int k, auto keys, auto values) {
     const int t0 = w.t0(k);
     const int r0 = w.row_begin(k), r1 = w.row_end(k);  // rows that some query sees, r0 < r1
-    const int blk = blk_next;
     if (even && r0 == t0 && r1 == t0 + 32) {
       size_t lo, up;
       if constexpr (PAGED) {
@@ -380,8 +395,10 @@ window_kernel(const WindowArgs a) {
       } else {
         lo = up = static_cast<size_t>(t0) * rstride;
       }
-      EvenCopy<C, STEPS, PAGED>::rows(Kb + lo, Kb + up, row_step, static_cast<int>(rstride), dma);
-      EvenCopy<C, STEPS, PAGED>::rows(Vb + lo, Vb + up, row_step, static_cast<int>(rstride), dma + C::SUB_ROWS_BYTES);
+      if constexpr (keys.value)
+        EvenCopy<C, STEPS, PAGED>::rows(Kb + lo, Kb + up, row_step, static_cast<int>(rstride), k_block);
+      if constexpr (values.value)
+        EvenCopy<C, STEPS, PAGED>::rows(Vb + lo, Vb + up, row_step, static_cast<int>(rstride), v_block);
     } else {
       // (addresses computed here, not kept in registers through the loop)
       int ln = lane;
@@ -397,28 +414,49 @@ window_kernel(const WindowArgs a) {
         else
           off[j] = static_cast<size_t>(pos) * rstride + piece;
       }
+      if constexpr (keys.value) {
 #pragma unroll
-      for (int j = 0; j < C::COPIES; ++j)
-        __builtin_amdgcn_global_load_lds((global_void*)(Kb + off[j]), (lds_void*)(dma + 1024 * j), 16, 0, kCopyPolicy);
+        for (int j = 0; j < C::COPIES; ++j)
+          __builtin_amdgcn_global_load_lds((global_void*)(Kb + off[j]), (lds_void*)(k_block + 1024 * j), 16, 0, kCopyPolicy);
+      }
+      if constexpr (values.value) {
 #pragma unroll
-      for (int j = 0; j < C::COPIES; ++j)
-        __builtin_amdgcn_global_load_lds((global_void*)(Vb + off[j]), (lds_void*)(dma + C::SUB_ROWS_BYTES + 1024 * j), 16,
-                                         0, kCopyPolicy);
+        for (int j = 0; j < C::COPIES; ++j)
+          __builtin_amdgcn_global_load_lds((global_void*)(Vb + off[j]), (lds_void*)(v_block + 1024 * j), 16, 0, kCopyPolicy);
+      }
     }
-    blk_next = blocks_of(k + kWinWaves);
   };
-  if (k < k1) request(k);
+  constexpr std::true_type yes;
+  constexpr std::false_type no;
+  // Memory operations of this wave complete in the order of their issue: K's copies, the
+  // block ids, the logits of the tile before, V's copies. A wait names how many issued
+  // after what it waits for may be left; block ids are not counted, as not every tile
+  // loads them.
+  constexpr int LEFT = C::COPIES + (SUMS ? 1 : 0);
+  if (k < k1) {
+    blk_next = blocks_of(k + kWinWaves);
+    request(k, yes, yes);
+    __builtin_amdgcn_s_waitcnt(wait_vm(C::COPIES));
+  }
   while (k < k1) {
     const int t0 = w.t0(k);
-    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __builtin_amdgcn_s_waitcnt(wait_vm(LEFT));  // K
 
     // the products q.K, unscaled
     float z[8];
     {
-      const f32x4 c0 = score_rows<DT, D>(lds, 0, qf, a4, n16);
-      const f32x4 c1 = score_rows<DT, D>(lds, 1, qf, a4, n16);
+      const f32x4 c0 = score_rows<DT, D>(kb, 0, qf, a4, n16);
+      const f32x4 c1 = score_rows<DT, D>(kb, 1, qf, a4, n16);
 #pragma unroll
       for (int i = 0; i < 8; ++i) z[i] = i < 4 ? c0[i & 3] : c1[i & 3];
+    }
+    const bool more = k + kWinWaves < k1;
+    // LDS reads of K have returned before the next tile's copies overwrite it
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+    if (more) {
+      blk = blk_next;
+      request(k + kWinWaves, yes, no);
+      blk_next = blocks_of(k + 2 * kWinWaves);
     }
     // value i of this lane is row t0 + pv_token(a4, i). Does every query see every row?
     const int last0 = w.L - a.T;                                     // the first query's own position
@@ -461,7 +499,8 @@ window_kernel(const WindowArgs a) {
       p[i] = (seen >> i) & 1u ? weight_of(a, z[i], m) : 0.f;
       l += p[i];
     }
-    const unsigned char* vb = lds + C::SUB_ROWS_BYTES;
+    if (more) __builtin_amdgcn_s_waitcnt(wait_vm(LEFT));  // V
+    else __builtin_amdgcn_s_waitcnt(kWaitVm0);
     if (!edge) {
       value_product<DT, D, C::ACC_N, true>(acc, vb, p, a4, n16);
     } else {
@@ -489,21 +528,19 @@ window_kernel(const WindowArgs a) {
       }
     }
     k += kWinWaves;
-    // LDS reads of the tile have returned before the next one's copies overwrite it
-    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
-    if (k < k1) request(k);
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);  // (V likewise)
+    if (more) request(k, no, yes);
   }
   l = sum_over_quads(l);
 
   // ---- join the four waves ----
-  constexpr int PITCH = D + 4;  // accumulator rows start on different banks
-  static_assert(16 * PITCH * 4 <= Q::BYTES, "accumulator rows of a wave");
+  constexpr int PITCH = Q::PITCH;
   __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
   if (a4 == 0) {
     ws.m[wave][n16] = m;
     ws.l[wave][n16] = l;
   }
-  store_acc<DT, D, C::ACC_N>(reinterpret_cast<float*>(lds) + n16 * PITCH, acc, a4);
+  store_acc<DT, D, C::ACC_N>(reinterpret_cast<float*>(lds_k + wave * Q::K_BYTES) + n16 * PITCH, acc, a4);
   __syncthreads();
   const size_t pair = static_cast<size_t>(b) * a.Hkv + g;
   const size_t piece0 = static_cast<size_t>(blockIdx.x) * TG;
@@ -518,7 +555,7 @@ window_kernel(const WindowArgs a) {
 #pragma unroll
     for (int v = 0; v < kWinWaves; ++v) {
       const float f = weight_of(a, ws.m[v][h], M);
-      const float4 x = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(lds_block + v * Q::BYTES) + h * PITCH)[c];
+      const float4 x = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(lds_k + v * Q::K_BYTES) + h * PITCH)[c];
       den = fmaf(f, ws.l[v][h], den);
       o.x = fmaf(f, x.x, o.x);
       o.y = fmaf(f, x.y, o.y);
