@@ -716,15 +716,17 @@ WindowPlan make_window_plan(const vp_shape& s, const vp_window& w, bool sums) {
   const int64_t pairs = static_cast<int64_t>(s.batch) * s.n_kv_heads;
   // One work-group per pair, and no second launch, where
   // * the walks are short: up to 16 tiles, 12 with sums (bf16; 8 KV heads of 128, 16 tiles:
-  //   9.2 us and, dealt, 12.1; with sums 11.3 and 12.0, 32 pairs 12.8 and 12.2; 32 tiles
-  //   15.3 and 12.1), 8 in fp32 (32 pairs of 128, 16 tiles: 19.6 and 15.2);
+  //   9.2 us and, dealt, 10.0; with sums 11.2 and 10.7, 32 pairs 12.9 and 10.9; 32 tiles
+  //   13.8 and 10.2), 8 in fp32 (32 pairs of 128: 13.5 and 14.1, 16 tiles 19.7 and 14.5);
   // * a window makes the walks of a batch much the same and the pairs nearly fill the CUs:
-  //   192 pairs (16 tiles: 12.7 and 16.2, 256 tiles: 117 and 133; 128 pairs, 64 tiles: 30.2
-  //   and 28.0), 384 with rows of 128 bytes (64 tiles: 35.9 and 41.7; 256 pairs: 31.3 and 28.2);
+  //   192 pairs (16 tiles: 11.3 and 16.3, 256 tiles: 115 and 130; 128 pairs, 64 tiles: 27.5
+  //   and 27.1), 384 with rows of 128 bytes (64 tiles: 35.1 and 37.7; 256 pairs: 29.3 and
+  //   27.5), 512 with their sums (64 tiles: 50.8 and 64.2; 384 pairs 47.2 and 45.1, 256
+  //   tiles 181 and 158);
   // * there are pairs for several rounds whatever their lengths: 1024.
   const bool bf16 = s.dtype == VP_BF16;
   const int64_t few = bf16 ? (sums ? 12 : 16) : 8;
-  const int64_t many = w.window == 0 ? 1024 : bf16 && s.head_dim == 64 ? 384 : 192;
+  const int64_t many = w.window == 0 ? 1024 : !bf16 || s.head_dim != 64 ? 192 : sums ? 512 : 384;
   const bool one_each = tiles <= few || pairs >= many || pairs * tiles > 0x3fffffff;
   // Otherwise one resident round of work-groups, a tile per wave at least; twice as many
   // as pairs where those are more (24 ragged sequences of 16 heads of 64: 51.5 us, four

@@ -116,6 +116,16 @@ def test_larger_batches(dtype, B, T, Hq, Hkv, d, cap, window, n_sink, page):
     check(q, K, V, lens, window, n_sink, dtype, page=page)
 
 
+@pytest.mark.parametrize("dtype,B,Hkv,d", [("bf16", 50, 8, 64), ("bf16", 66, 8, 64), ("bf16", 25, 8, 128),
+                                           ("f32", 23, 8, 64), ("f32", 25, 8, 64)])
+def test_windows_of_many_pairs(dtype, B, Hkv, d):
+    """Batches on both sides of the numbers of pairs from which a work-group takes a whole
+    window (of 20 tiles)."""
+    q, K, V = draw(B, B, 1, Hkv, Hkv, d, 680, dtype)
+    lens = np.random.default_rng(B).integers(0, 681, B).tolist()
+    check(q, K, V, lens, 600, 4, dtype)
+
+
 def test_more_pairs_than_work_groups():
     """600 (sequence, KV head) pairs: one part each, finished in one launch."""
     q, K, V = draw(1, 150, 1, 8, 4, 64, 90, "bf16")
