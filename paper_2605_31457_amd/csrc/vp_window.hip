@@ -231,16 +231,25 @@ struct StoreLogits {
   }
 };
 
-// One row of the walk on its way to its weight: row i is row i % 32 of tile i / 32
+// One row of the walk on its way to its weight: row i is row i % 32 of tile i / 32.
+// Only the queries that see the row add to it, by its position: a query with a NaN or
+// +inf logit has a NaN for 1 / sum, which a weight of 0 would not keep out.
 template <int GP>
 struct RowWeight {
   float z[GP];  // its products q.K
   float old;    // its sum so far
   float* dst;   // null: no row that a query sees
+  int h0, h1;   // query rows that see it
   __device__ __forceinline__ RowWeight(const WindowArgs& a, const WindowWalk& w, size_t pair, int i) : dst(nullptr) {
     const int k = i >> 5;
     const int j = w.t0(k) + (i & 31);
     if (k >= w.n || j < w.row_begin(k) || j >= w.row_end(k)) return;
+    // (where the sinks' and the window's tiles meet, rows that no query sees lie between)
+    const int own = j - (w.L - a.T);  // the query whose position it is
+    const int t0 = max(0, own), t1 = a.window == 0 || j < w.S ? a.T : min(a.T, own + a.window);
+    if (t0 >= t1) return;
+    h0 = t0 * a.G;
+    h1 = t1 * a.G;
     const float* src = a.zs + (pair * a.tiles * 32 + i) * GP;
     if constexpr (GP >= 4) {
 #pragma unroll
@@ -264,7 +273,7 @@ struct RowWeight {
     float s = 0.f;
 #pragma unroll
     for (int h = 0; h < GP; ++h)
-      if (h < a.T * a.G) s = fmaf(weight_of(a, z[h], norm[h].x), norm[h].y, s);
+      if (h >= h0 && h < h1) s = fmaf(weight_of(a, z[h], norm[h].x), norm[h].y, s);
     *dst = old + s;
   }
 };
