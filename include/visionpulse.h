@@ -399,7 +399,10 @@ vp_status vp_evict_workspace_size(const vp_shape* shape, const vp_evict_params* 
  * lists per sequence), the score being its attn_sum. VP_SCOPE_SEQUENCE: one set
  * of rows for all KV heads (U = 1), the score being the sum of attn_sum over
  * the KV heads (added in double, rounded once to float). A NaN sum counts as
- * the largest.
+ * the largest. The scope is this call's own: steps with budgets per KV group
+ * may evict with VP_SCOPE_SEQUENCE, and need to where sequences have visual
+ * tokens, since a row's position then differs by head and layout->vis_seg means
+ * nothing after an eviction per KV head.
  *
  *   kept         int32 [B*U, C]: positions (before the call) of the rows that
  *                stay, ascending, then -1

@@ -173,21 +173,28 @@ class DeviceStep:
         vp.vp_window_decode_attn(self.shape, self.layout, opt, self.q, self.K, self.V, self.attn_sum if sums else None,
                                  self.out, ws, nbytes, stream)
 
-    def evict(self, budget, n_sink=0, n_recent=0, stream=None):
+    def evict(self, budget, n_sink=0, n_recent=0, stream=None, kv_groups=None):
         """vp_evict in place, by ``attn_sum``: K, V, attn_sum and seq_len of every
-        sequence of more than ``budget`` rows, and the visual segments (with one kept
-        set per sequence). Returns the kept positions [B * (1 or Hkv), budget]. With
-        ``kv_groups`` every KV head keeps its own rows, and segments would differ by
-        head: sequences with visual tokens need the method's one set."""
+        sequence of more than ``budget`` rows, and the visual segments. Returns the kept
+        positions [B * (1 or Hkv), budget]. ``kv_groups``: every KV head keeps its own
+        rows, else one set per sequence (None: as the step's budgets are). A sequence's
+        segments cannot name rows that differ by head: with visual tokens only one set
+        per sequence is taken."""
         if self.attn_sum is None:
             raise RuntimeError("evict: no attention sums yet (window_decode_attn(sums=True) accumulates them)")
+        groups = self.kv_groups if kv_groups is None else kv_groups
+        if groups and any(n > 0 for segs in self.w.segments for _, n in segs):
+            raise RuntimeError("evict: the visual segments of rows that every KV head keeps for itself would differ by "
+                               "head (kv_groups=False keeps one set per sequence)")
+        shape = vp.vp_shape.from_buffer_copy(self.shape)
+        shape.scope = vp.VP_SCOPE_KV_GROUP if groups else vp.VP_SCOPE_SEQUENCE
         opt = vp.vp_evict_params(budget=budget, n_sink=n_sink, n_recent=n_recent)
-        nbytes = vp.vp_evict_workspace_size(self.shape, opt)
+        nbytes = vp.vp_evict_workspace_size(shape, opt)
         with self._order_of(stream):
-            kept = torch.empty(self.w.B * self.rows, budget, dtype=torch.int32, device=self.device)
+            kept = torch.empty(self.w.B * (self.w.Hkv if groups else 1), budget, dtype=torch.int32, device=self.device)
             ws = self._workspace(nbytes)
-        vp.vp_evict(self.shape, self.layout, opt, self.attn_sum, self.K, self.V, kept, self.attn_sum,
-                    None if self.kv_groups else self.seg, self.seq_len, ws, nbytes, stream)
+        vp.vp_evict(shape, self.layout, opt, self.attn_sum, self.K, self.V, kept, self.attn_sum,
+                    None if groups else self.seg, self.seq_len, ws, nbytes, stream)
         return kept
 
     def run(self, fused=True, stream=None):
