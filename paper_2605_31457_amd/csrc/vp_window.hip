@@ -727,16 +727,26 @@ WindowPlan make_window_plan(const vp_shape& s, const vp_window& w, bool sums) {
   // * the walks are short: up to 16 tiles, 12 with sums (bf16; 8 KV heads of 128, 16 tiles:
   //   9.2 us and, dealt, 10.0; with sums 11.2 and 10.7, 32 pairs 12.9 and 10.9; 32 tiles
   //   13.8 and 10.2), 8 in fp32 (32 pairs of 128: 13.5 and 14.1, 16 tiles 19.7 and 14.5);
-  // * a window makes the walks of a batch much the same and the pairs nearly fill the CUs:
-  //   192 pairs (16 tiles: 11.3 and 16.3, 256 tiles: 115 and 130; 128 pairs, 64 tiles: 27.5
-  //   and 27.1), 384 with rows of 128 bytes (64 tiles: 35.1 and 37.7; 256 pairs: 29.3 and
-  //   27.5), 512 with their sums (64 tiles: 50.8 and 64.2; 384 pairs 47.2 and 45.1, 256
-  //   tiles 181 and 158);
-  // * there are pairs for several rounds whatever their lengths: 1024.
+  // * the longest walk is short beside the batch, a tile for 8 pairs at most: then one
+  //   full sequence among short ones costs no more than the deal (bf16 of 128, no window;
+  //   1024 pairs: 128 tiles, all full 311 and 336 us, one full 93 and 109; 256 tiles 616 and
+  //   644, 123 and 111, with sums 875 and 911, 196 and 146; 1024 tiles, one full 338 and 129,
+  //   with sums 599 and 174; 512 pairs: 64 tiles 83 and 92, 36 and 38, 128 tiles 158 and 167,
+  //   53 and 39; 192 pairs: 32 tiles 18.2 and 23.7, 14.0 and 14.4, 64 tiles 33 and 40, 24 and 18);
+  // * a window cuts the walks of the capacity to half or less, so that long sequences' are
+  //   much the same, and the pairs nearly fill the CUs: 192 pairs (16 tiles: 11.3 and 16.3,
+  //   256 tiles: 115 and 130; 128 pairs, 64 tiles: 27.5 and 27.1), 384 with rows of 128 bytes
+  //   (64 tiles: 35.1 and 37.7; 256 pairs: 29.3 and 27.5), 512 with their sums (64 tiles: 50.8
+  //   and 64.2; 384 pairs 47.2 and 45.1, 256 tiles 181 and 158). Where nearly all sequences
+  //   are shorter than such a window this loses: window 8192, 256 pairs, one context of 32k
+  //   among some of 1k 82 us and, dealt, 34; of 1k to 32k 144 and 151. A window that the
+  //   capacity hardly exceeds, or does not, cuts nothing (24 contexts of 1k to 32k, 8 KV heads,
+  //   window 32768: 328 us and, dealt, 233).
   const bool bf16 = s.dtype == VP_BF16;
   const int64_t few = bf16 ? (sums ? 12 : 16) : 8;
-  const int64_t many = w.window == 0 ? 1024 : !bf16 || s.head_dim != 64 ? 192 : sums ? 512 : 384;
-  const bool one_each = tiles <= few || pairs >= many || pairs * tiles > 0x3fffffff;
+  const int64_t many = !bf16 || s.head_dim != 64 ? 192 : sums ? 512 : 384;
+  const bool cut = w.window > 0 && 2 * tiles <= cap;
+  const bool one_each = tiles <= few || 8 * tiles <= pairs || (cut && pairs >= many) || pairs * tiles > 0x3fffffff;
   // Otherwise one resident round of work-groups, a tile per wave at least; twice as many
   // as pairs where those are more (24 ragged sequences of 16 heads of 64: 51.5 us, four
   // times as many 53.1)
