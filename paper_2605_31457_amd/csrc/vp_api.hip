@@ -773,7 +773,8 @@ vp_status vp_window_decode_attn(const vp_shape* shape, const vp_layout* layout, 
   a.window = std::min(window->window, 2 * kMaxTokens);  // (further back than any row)
   a.n_sink = window->n_sink;
   const float sm = window->sm_scale > 0.f ? window->sm_scale : 1.0f / std::sqrt(static_cast<float>(shape->head_dim));
-  a.zscale = sm * 1.4426950408889634f;  // log2(e)
+  // log2(e); the largest scales stay finite, as an infinite one makes a NaN of the maximum's weight
+  a.zscale = std::min(sm * 1.4426950408889634f, 0x1.fffffep127f);
   // weights stay below 2^8, and rescaling is rare; small beside the maximum that precedes
   // the first row (-FLT_MAX), which every product exceeds
   a.raise = std::min(8.f / a.zscale, 0x1p100f);
