@@ -128,6 +128,13 @@ def _on_current_device(fn, *args):
             raise ValueError(f"{fn}: a tensor is on {x.device}, the current device is cuda:{here}")
 
 
+def _room(workspace, workspace_bytes):
+    """Bytes of a workspace, which a call that needs none takes as None."""
+    if workspace_bytes is not None:
+        return workspace_bytes
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
 def _check(fn, status):
     if status != 0:
         raise VPError(fn, status, lib().vp_last_error().decode())
@@ -250,7 +257,7 @@ def vp_window_decode_attn(shape, layout, window, q, K, V, attn_sum, out, workspa
     """Attention over a sliding window and the first tokens; attn_sum None, or
     float32 [B, Hkv, max_seq_len] to which the rows' weights are added."""
     _on_current_device("vp_window_decode_attn", q, K, V, attn_sum, out, workspace)
-    nbytes = workspace.numel() * workspace.element_size() if workspace_bytes is None else workspace_bytes
+    nbytes = _room(workspace, workspace_bytes)
     _check("vp_window_decode_attn", lib().vp_window_decode_attn(
         ctypes.byref(shape), ctypes.byref(layout), ctypes.byref(window), _p(q), _p(K), _p(V), _p(attn_sum), _p(out),
         _p(workspace), nbytes, _stream(stream)))
@@ -269,7 +276,7 @@ def vp_evict(shape, layout, params, attn_sum, K, V, kept, attn_sum_out, vis_seg_
     place; vis_seg_out may be None. attn_sum_out, vis_seg_out and new_len may be the
     arrays that attn_sum and the layout name."""
     _on_current_device("vp_evict", attn_sum, K, V, kept, attn_sum_out, vis_seg_out, new_len, workspace)
-    nbytes = workspace.numel() * workspace.element_size() if workspace_bytes is None else workspace_bytes
+    nbytes = _room(workspace, workspace_bytes)
     _check("vp_evict", lib().vp_evict(
         ctypes.byref(shape), ctypes.byref(layout), ctypes.byref(params), _p(attn_sum), _p(K), _p(V), _p(kept),
         _p(attn_sum_out), _p(vis_seg_out), _p(new_len), _p(workspace), nbytes, _stream(stream)))
