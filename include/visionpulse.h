@@ -330,7 +330,7 @@ vp_status vp_decode_step_static(const vp_shape* shape, const vp_layout* layout, 
  * attention of layers (or steps) that look at a window of it, and the eviction
  * of rows that attention no longer goes to. A loop that holds its caches to C
  * rows appends its tokens, calls vp_window_decode_attn with attn_sum, and calls
- * vp_evict whenever the caches have grown some way past C. Both use shape and
+ * vp_evict for every layer's caches whenever they have grown some way past C. Both use shape and
  * layout as the other calls do (vp_window_decode_attn reads no visual segments
  * and takes them as NULL).
  */
@@ -367,7 +367,9 @@ vp_status vp_window_workspace_size(const vp_shape* shape, const vp_window* windo
  * all heads of its KV group; rows that none sees, and entries from seq_len on,
  * are left as they are. The rows of the queries themselves (the last T
  * positions) are new: their entries start from zero whatever they hold, so a
- * loop never clears them. The weights are added in a fixed order: the same
+ * loop need not clear them. The entries of rows that were in the cache before
+ * the first such call (a prompt's) are added to like all others: give them the
+ * prompt's weights, or zeros. The weights are added in a fixed order: the same
  * call on the same inputs gives the same bits.
  *
  * layout: seq_len (and block_table with paged caches); the segments are not
@@ -414,6 +416,14 @@ vp_status vp_evict_workspace_size(const vp_shape* shape, const vp_evict_params* 
  *                0, which the decode-step calls accept). May be layout->vis_seg.
  *                VP_SCOPE_SEQUENCE only (VP_ERR_UNSUPPORTED otherwise).
  *   new_len      int32 [B]: min(seq_len, C). May be layout->seq_len.
+ *
+ * Several layers. A call compacts one layer's caches, and the rows it keeps
+ * depend on attn_sum, seq_len, params and scope alone. Layers that share lengths
+ * and segments, or follow another's vis_idx (positions in the caches), must lose
+ * the same rows: call vp_evict for each layer's K and V with one attn_sum (a
+ * layer's, or the layers' added up), and give attn_sum_out, vis_seg_out and
+ * new_len arrays of their own in every call but the last. Written in place by
+ * an earlier one, they leave the later ones nothing to evict.
  *
  * Rows from new_len on, of K, V and attn_sum_out, are left as they are. The
  * visual segments are read only for vis_seg_out. A block that two sequences
