@@ -219,6 +219,16 @@ struct EvenCopy {
   }
 };
 
+// A float to the stage. Written by hand, because the compiler may have any LDS store wait
+// for all copies in flight (fp32 rows of 128, 8 x 16k with sums: 111 us, so 108). A wave's LDS
+// accesses happen in order, so its reads of the stage need nothing else.
+__device__ __forceinline__ void stage_store(float* p, float x) {
+#ifdef __HIP_DEVICE_COMPILE__
+  typedef __attribute__((address_space(3))) float lds_float;
+  asm volatile("ds_write_b32 %0, %1" ::"v"((uint32_t)(uintptr_t)(lds_float*)p), "v"(x) : "memory");
+#endif
+}
+
 // a tile's logits, 32 rows of gp floats, from the stage to the plane
 struct StoreLogits {
   static __device__ __forceinline__ void tile(float* dst, const float* stage, int gp, int lane) {
@@ -484,7 +494,7 @@ window_kernel(const WindowArgs a) {
       const int gp = a.gp;
       if (n16 < gp) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) stage[pv_token(a4, i) * gp + n16] = (seen >> i) & 1u ? z[i] : kNegInf;
+        for (int i = 0; i < 8; ++i) stage_store(stage + pv_token(a4, i) * gp + n16, (seen >> i) & 1u ? z[i] : kNegInf);
       }
       StoreLogits::tile(zplane + static_cast<size_t>(k) * 32 * gp, stage, gp, lane);
     }
