@@ -413,7 +413,8 @@ vp_status vp_evict_workspace_size(const vp_shape* shape, const vp_evict_params* 
  *                new_len; later entries are left as they are. May be attn_sum.
  *   vis_seg_out  NULL, or int32 [n_seg][2] like layout->vis_seg: the segments of
  *                the compacted sequence (one that lost all its rows has length
- *                0, which the decode-step calls accept). May be layout->vis_seg.
+ *                0, which the decode-step calls accept and vp_validate_layout
+ *                reports). May be layout->vis_seg.
  *                VP_SCOPE_SEQUENCE only (VP_ERR_UNSUPPORTED otherwise).
  *   new_len      int32 [B]: min(seq_len, C). May be layout->seq_len.
  *

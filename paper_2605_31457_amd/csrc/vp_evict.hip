@@ -207,9 +207,10 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(const EvictAr
 }
 
 constexpr int kMoveThreads = 256;
-// Rows per work-group: 128 KB of K and V (32 x 32k tokens: 64 rows of 256 bytes 627 us per
-// call, 128 494, 256 441), 32 KB where that would leave CUs idle (1 x 8k tokens: 18.1 us,
-// with 256 rows 19.7)
+// Rows per work-group: 128 KB of K and V of 256- and 512-byte rows (32 x 32k tokens: 64 rows
+// of 256 bytes 627 us per call, 128 494, 256 441), 32 KB where that would leave CUs idle
+// (1 x 8k tokens: 18.1 us, with 256 rows 19.7). Rows of 128 bytes: as many as of 256, half
+// the bytes, as a work-group has a thread for each row.
 constexpr int large_rows(int row_bytes) { return row_bytes > 256 ? 128 : 256; }
 constexpr int small_rows(int row_bytes) { return row_bytes > 256 ? 32 : 64; }
 

@@ -129,11 +129,11 @@ __device__ __forceinline__ int pv_token(int a4, int i) { return i < 4 ? 4 * a4 +
 // acc += V^T P^T over the tile's 32 rows. SPLIT (bf16): the weights enter as the sum
 // of three bf16 numbers, all 24 bits of them, instead of one of 8: the leading two
 // truncated, the rests positive where the weight is, so that an infinite value stays an
-// infinity of its sign (two, 16 bits, cost 0.3 to 1.5% less, 64 windows of 8k 159.0 us and
-// 160.4, and put 3 to 4 in 1000 bf16 outputs on the other side of a rounding, mostly the
-// wrong one; three do so for 5 to 10 in 10000, mostly the right one beside a product in
-// float32 of their own order). Bit i of `rows` (masked tiles): the row in this lane's slot
-// i takes part; the others count as zeros whatever they hold.
+// infinity of its sign. (Two, 16 bits, cost 0.3 to 1.5% less, 64 windows of 8k 159.0 us
+// and 159.6, and put 3 to 4 in 1000 bf16 outputs on the other side of a rounding than a
+// product in float32, mostly the wrong one; with three it is 5 to 17 in 10000, mostly the
+// right one.) Bit i of `rows` (masked tiles): the row in this lane's slot i takes part; the
+// others count as zeros whatever they hold.
 template <int DT, int D, int N, bool SPLIT = false, bool MASKED = false>
 __device__ __forceinline__ void value_product(f32x4 (&acc)[N], const unsigned char* vb, const float (&p)[8],
                                               int a4, int n16, unsigned rows = 0xffu) {

@@ -21,8 +21,10 @@
 //                  every tile. A wave asks for a tile's K as soon as the products of the
 //                  one before are done and for its V when that one's values are in: asked
 //                  for together, after the values, fp32 rows wait for the matrix
-//                  instructions (8 paged caches of 4k to 9k tokens with sums 69 us, now 60;
-//                  4 of 32 heads 57, now 51; bf16, 64 windows of 8k 161, now 159). The waves' partials meet in LDS. With sums the logits
+//                  instructions (fp32, 8 paged caches of 4k to 9k tokens, 4 KV heads of 128
+//                  for 28, with sums: 252 MB in 69 us, now 60; 4 of 1k to 2.5k with 32 KV
+//                  heads: 245 MB in 57, now 51; bf16, 64 windows of 8k, 1083 MB: 161, now
+//                  159). The waves' partials meet in LDS. With sums the logits
 //                  leave as rows of gp floats (32 bytes per row at 7 heads, beside 512 of
 //                  K and V), since a weight is known only when the whole walk is. That
 //                  is what sums cost: any stores in a stream of reads slow the reads (16
