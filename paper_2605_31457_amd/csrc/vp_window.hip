@@ -739,12 +739,15 @@ WindowPlan make_window_plan(const vp_shape& s, const vp_window& w, bool sums) {
   // * the walks are short: up to 16 tiles, 12 with sums (bf16; 8 KV heads of 128, 16 tiles:
   //   9.2 us and, dealt, 10.0; with sums 11.2 and 10.7, 32 pairs 12.9 and 10.9; 32 tiles
   //   13.8 and 10.2), 8 in fp32 (32 pairs of 128: 13.5 and 14.1, 16 tiles 19.7 and 14.5);
-  // * the longest walk is short beside the batch, a tile for 8 pairs at most: then one
-  //   full sequence among short ones costs no more than the deal (bf16 of 128, no window;
-  //   1024 pairs: 128 tiles, all full 311 and 336 us, one full 93 and 109; 256 tiles 616 and
-  //   644, 123 and 111, with sums 875 and 911, 196 and 146; 1024 tiles, one full 338 and 129,
-  //   with sums 599 and 174; 512 pairs: 64 tiles 83 and 92, 36 and 38, 128 tiles 158 and 167,
-  //   53 and 39; 192 pairs: 32 tiles 18.2 and 23.7, 14.0 and 14.4, 64 tiles 33 and 40, 24 and 18);
+  // * the longest walk is short beside what dealing costs. A full sequence alone among short
+  //   ones holds the call for 0.3 us a tile; dealing takes pairs (350 + sequences) / 40000 us,
+  //   as every work-group reads all lengths before its rows. Dealt from five times that on.
+  //   bf16 of 128, no window, all full / 100 to 1500 rows / one full among those, whole and dealt:
+  //   192 pairs of 48 sequences, 32 tiles 18.2 and 23.7 / 16.3, 17.8 / 14.0, 14.4, 64 tiles
+  //   33, 40 / 27, 25 / 24, 18; 1024 of 128, 128 tiles 311, 336 / 72, 88 / 93, 109, 256 tiles 616,
+  //   644 / 72, 88 / 123, 111, 1024 tiles - / 71, 87 / 338, 129 (with sums 105, 120 / 599, 174);
+  //   2048 of 512, 1024 tiles - / 146, 186 / 541, 200; 4096 of 1024 - / 281, 423 / 600, 431; 4096
+  //   of 4096 - / 267, 726 / 583, 732;
   // * a window cuts the walks of the capacity to half or less, so that long sequences' are
   //   much the same, and the pairs nearly fill the CUs: 192 pairs (16 tiles: 11.3 and 16.3,
   //   256 tiles: 115 and 130; 128 pairs, 64 tiles: 27.5 and 27.1), 384 with rows of 128 bytes
@@ -758,7 +761,8 @@ WindowPlan make_window_plan(const vp_shape& s, const vp_window& w, bool sums) {
   const int64_t few = bf16 ? (sums ? 12 : 16) : 8;
   const int64_t many = !bf16 || s.head_dim != 64 ? 192 : sums ? 512 : 384;
   const bool cut = w.window > 0 && 2 * tiles <= cap;
-  const bool one_each = tiles <= few || 8 * tiles <= pairs || (cut && pairs >= many) || pairs * tiles > 0x3fffffff;
+  const bool brief = 2400 * tiles <= pairs * (350 + s.batch);
+  const bool one_each = tiles <= few || brief || (cut && pairs >= many) || pairs * tiles > 0x3fffffff;
   // Otherwise one resident round of work-groups, a tile per wave at least; twice as many
   // as pairs where those are more (24 ragged sequences of 16 heads of 64: 51.5 us, four
   // times as many 53.1)

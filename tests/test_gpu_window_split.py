@@ -9,18 +9,21 @@ from test_gpu_window import check, draw
 pytestmark = pytest.mark.gpu
 
 
-@pytest.mark.parametrize("dtype,T,B,Hkv,d", [("bf16", 1, 165, 2, 64), ("bf16", 2, 40, 8, 64), ("f32", 1, 40, 8, 64),
-                                             ("bf16", 1, 40, 8, 128)])
-@pytest.mark.parametrize("tiles,window", [(40, 0), (42, 0), (42, 2 ** 31 - 1), (42, 900), (42, 550)])
-def test_one_full_sequence_among_short_ones(dtype, T, B, Hkv, d, tiles, window):
-    cap = 32 * tiles - 5
-    q, K, V = draw(B + tiles, B, T, Hkv, Hkv, d, cap, dtype)
-    lens = np.random.default_rng(B).integers(0, 70, B).tolist()
-    lens[B // 2] = cap
-    check(q, K, V, lens, window, 4, dtype)
+@pytest.mark.parametrize("dtype,T,B,Hkv,d,whole,dealt", [("bf16", 1, 165, 2, 64, 69, 72), ("bf16", 2, 40, 8, 64, 51, 54),
+                                                         ("f32", 1, 40, 8, 64, 51, 54), ("bf16", 1, 40, 8, 128, 51, 54)])
+@pytest.mark.parametrize("window", [0, 2 ** 31 - 1, 1200, 700])
+def test_one_full_sequence_among_short_ones(dtype, T, B, Hkv, d, whole, dealt, window):
+    """Capacities on both sides of the one from which walks without a window (or with one that
+    cuts little) are dealt; 700 cuts them to half, and is taken whole either way."""
+    for tiles in (whole, dealt):
+        cap = 32 * tiles - 5
+        q, K, V = draw(B + tiles, B, T, Hkv, Hkv, d, cap, dtype)
+        lens = np.random.default_rng(B).integers(0, 70, B).tolist()
+        lens[B // 2] = cap
+        check(q, K, V, lens, window, 4, dtype)
 
 
-@pytest.mark.parametrize("tiles", [20, 26])
+@pytest.mark.parametrize("tiles", [32, 35])
 def test_lengths_of_every_size(tiles):
     cap = 32 * tiles
     q, K, V = draw(tiles, 50, 1, 8, 4, 64, cap, "bf16")

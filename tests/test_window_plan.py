@@ -27,5 +27,10 @@ def test_a_window_past_the_capacity_is_none(B, Hkv, cap, dtype, d, sums):
 def test_long_walks_of_many_pairs_are_shared_out():
     """One full context among short ones must not leave its pairs to a work-group each."""
     assert size(128, 8, 32768, 0) > 0 and size(256, 4, 32768, 0) > 0 and size(64, 4, 32768, 32000) > 0
-    assert size(128, 8, 1024, 0) == 0  # (short beside the batch)
+    assert size(512, 4, 32768, 0) > 0
+    # (short beside what dealing costs: few tiles, or lengths of many sequences to read)
+    assert size(128, 8, 1024, 0) == 0 and size(2048, 4, 32768, 0) == 0 and size(4096, 1, 32768, 0) == 0
+    # both sides of the capacities in test_gpu_window_split.py
+    for B, Hkv, d, whole, dealt in ((165, 2, 64, 69, 72), (40, 8, 64, 51, 54), (40, 8, 128, 51, 54), (50, 4, 64, 32, 35)):
+        assert size(B, Hkv, 32 * whole, 0, d=d) == 0 and size(B, Hkv, 32 * dealt, 0, d=d) > 0
     assert size(64, 4, 32768, 8192) == 0  # (a window that cuts them)
