@@ -310,7 +310,7 @@ def _to_4bit(x):
     y = x.unflatten(-1, (-1, 32))
     top = y.abs().amax(-1, keepdim=True)
     m, e = torch.frexp(top)
-    e = torch.where(m > 0.875, e - 2, e - 3).clamp(-125, 126)
+    e = torch.where(m > 0.875, e - 2, e - 3).clamp(-125, 125)
     e = torch.where(top == 0, -125, e)
     y = torch.ldexp(y.abs(), -e).unflatten(-1, (-1, 2))
     code = ((y > 0.25).to(torch.uint8) + (y >= 0.75) + (y > 1.25) + (y >= 1.75) + (y > 2.5) + (y >= 3.5) + (y > 5.0))
@@ -330,7 +330,7 @@ def _round4(x):
     top = y.abs().amax(-1, keepdim=True)
     scale = torch.exp2(torch.ceil(torch.log2(top.clamp(min=1e-300) / 7.0)))
     scale = torch.where(scale * 3.5 >= top, scale * 0.5, scale)  # (the logarithm's own rounding)
-    scale = torch.where(scale * 7.0 < top, scale * 2.0, scale).clamp(2.0 ** -125, 2.0 ** 126)
+    scale = torch.where(scale * 7.0 < top, scale * 2.0, scale).clamp(2.0 ** -125, 2.0 ** 125)
     y = y / scale
     a = y.abs()
     step = torch.where(a < 2.0, 0.5, torch.where(a < 4.0, 1.0, 2.0))
