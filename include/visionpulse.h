@@ -440,6 +440,118 @@ vp_status vp_evict(const vp_shape* shape, const vp_layout* layout, const vp_evic
                    int32_t* vis_seg_out, int32_t* new_len, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Filling caches, and caches held in 4 bits
+ * -----------------------------------------
+ * vp_append_kv puts new tokens into caches of the other calls; vp_append_kv4 puts
+ * them into a cache of 4 bits per element, a quarter of the bytes of bfloat16, over which
+ * vp_kv4_decode_attn attends and from which vp_kv4_read brings rows back.
+ * layout: seq_len counts the new tokens already, as it does for the step's attention
+ * (and block_table with paged caches); the segments are not read and may be NULL.
+ * shape.max_vis, max_segs, k_cap and scope have no effect.
+ */
+
+/* Rotation of queries and keys by position. Of every head the first rot_dim elements
+ * turn in pairs; pair i (of rot_dim / 2) is elements (i, i + rot_dim / 2), or with
+ * interleaved (2 i, 2 i + 1):
+ *   a' = a c - b s,  b' = b c + a s,    c = cos_sin[p][i], s = cos_sin[p][rot_dim / 2 + i]
+ * p is the token's position on the pair's axis, clipped to [0, n_pos). With one axis
+ * that is pos[token], or the token's cache row where pos is NULL. With several (an image's
+ * rows and columns beside time) pairs 0 .. section[0] - 1 take axis 0, the next
+ * section[1] axis 1, and so on. The remaining elements stay as they are. */
+typedef struct vp_rope {
+  const float* cos_sin;  /* device [n_pos][rot_dim]: cosines, then sines; 16-byte aligned */
+  int32_t n_pos;
+  int32_t rot_dim;       /* a multiple of 16, at most head_dim */
+  int32_t interleaved;   /* 0 or 1 */
+  int32_t n_axes;        /* 1 .. 4 */
+  const int32_t* pos;    /* device [n_axes][n_tokens]; NULL (one axis): cache rows */
+  int32_t section[4];    /* n_axes > 1: pairs of each axis, multiples of 4 that add up to rot_dim / 2 */
+} vp_rope;
+
+/* New tokens, one after another, those of a sequence together. Token i's heads lie at
+ * q + i * q_stride (elements of shape.dtype), next to each other: q, k and v may be
+ * columns of one product. Strides are multiples of 16 bytes. */
+typedef struct vp_tokens {
+  const void* q;           /* device [n_tokens][Hq][d], or NULL: no queries */
+  const void* k;           /* device [n_tokens][Hkv][d] */
+  const void* v;           /* device [n_tokens][Hkv][d] */
+  int64_t q_stride;
+  int64_t k_stride;
+  int64_t v_stride;
+  const int32_t* new_off;  /* device [B+1], ascending: sequence b has tokens new_off[b] .. new_off[b+1] - 1;
+                              NULL: n_queries tokens each */
+  int32_t n_tokens;        /* rows of q, k, v (those that new_off gives to no sequence are left alone) */
+} vp_tokens;
+
+/* A 4-bit cache. A row of d elements is d/2 bytes of codes, two elements a byte, the
+ * lower-numbered one in the low half: a sign bit over three bits that stand for 0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6; and d/32 scale bytes, one per 32 elements: element = code * 2^(scale - 127).
+ * Rows of a KV head follow each other: row s of KV head h of sequence b has its codes at
+ * b*code_stride_b + h*code_stride_h + s*d/2 and its scales at b*scale_stride_b +
+ * h*scale_stride_h + s*d/32 (bytes; paged: physical blocks and rows in them, as for the other
+ * caches, of 16 rows or more). Pointers and strides are multiples of 16. */
+typedef struct vp_kv4 {
+  void* k_codes;
+  void* k_scales;
+  void* v_codes;
+  void* v_scales;
+  int64_t code_stride_b;
+  int64_t code_stride_h;
+  int64_t scale_stride_b;
+  int64_t scale_stride_h;
+} vp_kv4;
+
+/*
+ * vp_append_kv -- the n tokens of every sequence go to its last n rows: K gets k rotated,
+ * V gets v, and q_out [n_tokens, Hq, d] gets q rotated (rope NULL: as it is). q_out may be q
+ * where q's tokens follow each other without gaps, and must not overlap it otherwise; with
+ * n_queries tokens each it is the q of the step's other calls. The rotation is done in
+ * 64 bits and rounded to the caches' type (bfloat16 through float). Tokens whose row would
+ * lie before row 0 (a sequence shorter than its new tokens) are left out, their queries
+ * too. Nothing else in the caches and in q_out is written.
+ * The caches' rows must not overlap (VP_ERR_SHAPE for strides that make them), nor the
+ * inputs; two sequences that share the block they append to write over each other.
+ */
+vp_status vp_append_kv(const vp_shape* shape, const vp_layout* layout, const vp_rope* rope, const vp_tokens* tokens,
+                       void* q_out, void* K, void* V, void* stream);
+
+/*
+ * vp_append_kv4 -- vp_append_kv into a 4-bit cache. Of 32 elements with largest magnitude
+ * m the scale is the least power of two of which m is at most seven times (2^-125 at
+ * least, 2^125 at most), and every code the one nearest to element / scale, ties to the
+ * even code, at most 6: an element is off by half a step of its code, a quarter of it at most where
+ * it is above the scale, and 0.25 of the scale below. Codes are those of the 64-bit values. 32 elements among which
+ * is an infinity or NaN become NaN, all of them (scale byte 255). shape's K and V strides
+ * have no effect. The rows of a cache must not overlap (VP_ERR_SHAPE).
+ * VP_ERR_UNSUPPORTED: block_size below 16.
+ */
+vp_status vp_append_kv4(const vp_shape* shape, const vp_layout* layout, const vp_rope* rope, const vp_tokens* tokens,
+                        void* q_out, const vp_kv4* cache, void* stream);
+
+/*
+ * vp_kv4_read -- rows first[b] .. seq_len[b] - 1 (first NULL: all) of a 4-bit cache into
+ * caches of shape.dtype, at the same positions: exactly what the codes stand for. Paged
+ * caches share the block table. Other rows of K and V are left as they are. The decode step's calls run
+ * on what it writes. Scale bytes are those of vp_append_kv4 (2 .. 252, 255).
+ */
+vp_status vp_kv4_read(const vp_shape* shape, const vp_layout* layout, const vp_kv4* cache, const int32_t* first, void* K,
+                      void* V, void* stream);
+
+/* Bytes of device workspace vp_kv4_decode_attn needs; 0 bytes: none, and NULL will do. A
+ * workspace for a larger call is not always large enough: ask for each shape. */
+vp_status vp_kv4_workspace_size(const vp_shape* shape, const vp_window* window, size_t* bytes);
+
+/*
+ * vp_kv4_decode_attn -- vp_window_decode_attn (without sums) over a 4-bit cache: the same
+ * positions seen, [B, T, Hq, d] in and out, zeros for a query that sees nothing or whose
+ * logits are all -inf, no influence of rows that a query does not see. Products and sums are formed in 32 bits
+ * from the values that the codes stand for. Strides of K and V in shape have no effect.
+ * The workspace must not be shared by concurrent calls.
+ */
+vp_status vp_kv4_decode_attn(const vp_shape* shape, const vp_layout* layout, const vp_window* window, const void* q,
+                             const vp_kv4* cache, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * vp_step_plan -- how vp_visual_mass and vp_decode_step will launch
  * their kernels for this shape (pure host computation; for profiling and
  * benchmarks). flags is a bit set of

@@ -12,6 +12,7 @@
 
 #include "vp_cache.h"
 #include "vp_internal.h"
+#include "vp_kv4.h"
 
 // Scratch memory of vp_decode_step_static: each GPU the library runs on holds
 // one copy of this array until the process ends. Host code never uses its name
@@ -355,6 +356,160 @@ vp_status check_room(void* ws, size_t bytes, size_t need) {
   if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return fail(VP_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   if (bytes < need) return fail(VP_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", bytes, need);
   return VP_OK;
+}
+
+// Arguments of attention over a window (attn_sum and the caches' own are the caller's)
+WindowArgs window_args(const vp_shape* shape, const vp_layout* layout, const vp_window* window, const WindowPlan& plan,
+                       char* ws, const void* q, void* out) {
+  WindowArgs a{};
+  a.q = q;
+  a.out = out;
+  a.bs_log2 = -1;
+  if (shape->block_size > 0) {
+    a.bs_log2 = __builtin_ctz(static_cast<unsigned>(shape->block_size));
+    a.nblk = (shape->max_seq_len + shape->block_size - 1) / shape->block_size;
+    a.block_table = layout->block_table;
+  }
+  a.seq_len = layout->seq_len;
+  a.B = shape->batch;
+  a.Hq = shape->n_q_heads;
+  a.Hkv = shape->n_kv_heads;
+  a.G = shape->n_q_heads / shape->n_kv_heads;
+  a.T = queries(*shape);
+  a.max_seq_len = shape->max_seq_len;
+  a.window = std::min(window->window, 2 * kMaxTokens);  // (further back than any row)
+  a.n_sink = window->n_sink;
+  const float sm = window->sm_scale > 0.f ? window->sm_scale : 1.0f / std::sqrt(static_cast<float>(shape->head_dim));
+  // log2(e); the largest scales stay finite, as an infinite one makes a NaN of the maximum's weight
+  a.zscale = std::min(sm * 1.4426950408889634f, 0x1.fffffep127f);
+  // weights stay below 2^8, and rescaling is rare; small beside the maximum that precedes
+  // the first row (-FLT_MAX), which every product exceeds
+  a.raise = std::min(8.f / a.zscale, 0x1p100f);
+  a.tiles = plan.tiles;
+  a.groups = plan.groups;
+  a.gp = plan.gp;
+  a.stats = reinterpret_cast<float*>(ws + plan.stats);
+  a.acc = reinterpret_cast<float*>(ws + plan.acc);
+  a.pieces = reinterpret_cast<int2*>(ws + plan.pieces);
+  a.zs = reinterpret_cast<float*>(ws + plan.zs);
+  return a;
+}
+
+// Host checks of the calls that fill caches and of 4-bit caches.
+vp_status check_rope(const vp_shape* s, const vp_rope* r) {
+  if (!r) return VP_OK;  // (no rotation)
+  if (!r->cos_sin) return fail(VP_ERR_NULL, "rope cos_sin is NULL");
+  if (!aligned16(r->cos_sin)) return fail(VP_ERR_SHAPE, "cos_sin must be 16-byte aligned");
+  if (r->n_pos < 1 || r->n_pos > kMaxTokens) return fail(VP_ERR_RANGE, "n_pos %d outside [1, %d]", r->n_pos, kMaxTokens);
+  if (r->rot_dim < 16 || r->rot_dim > s->head_dim || r->rot_dim % 16 != 0)
+    return fail(VP_ERR_SHAPE, "rot_dim %d: a multiple of 16 in [16, head_dim %d]", r->rot_dim, s->head_dim);
+  if (r->interleaved != 0 && r->interleaved != 1) return fail(VP_ERR_RANGE, "interleaved must be 0 or 1");
+  if (r->n_axes < 1 || r->n_axes > kMaxAxes) return fail(VP_ERR_RANGE, "n_axes %d outside [1, %d]", r->n_axes, kMaxAxes);
+  if (reinterpret_cast<uintptr_t>(r->pos) & 3u) return fail(VP_ERR_SHAPE, "pos must be 4-byte aligned");
+  if (r->n_axes == 1) return VP_OK;
+  if (!r->pos) return fail(VP_ERR_NULL, "n_axes %d needs pos", r->n_axes);
+  int64_t sum = 0;
+  for (int i = 0; i < r->n_axes; ++i) {
+    if (r->section[i] < 0 || r->section[i] % 4 != 0)
+      return fail(VP_ERR_SHAPE, "section[%d] = %d: a multiple of 4 pairs, >= 0", i, r->section[i]);
+    sum += r->section[i];
+  }
+  if (sum != r->rot_dim / 2)
+    return fail(VP_ERR_SHAPE, "sections add up to %lld pairs, rot_dim / 2 is %d", static_cast<long long>(sum), r->rot_dim / 2);
+  return VP_OK;
+}
+
+vp_status check_tokens(const vp_shape* s, const vp_tokens* t, const void* q_out) {
+  if (!t) return fail(VP_ERR_NULL, "tokens is NULL");
+  if (!t->k || !t->v) return fail(VP_ERR_NULL, "tokens k and v required");
+  if (!t->q != !q_out) return fail(VP_ERR_NULL, "q and q_out: both or neither");
+  if (!aligned16(t->q) || !aligned16(t->k) || !aligned16(t->v) || !aligned16(q_out))
+    return fail(VP_ERR_SHAPE, "q, k, v, q_out must be 16-byte aligned");
+  const int64_t step = s->dtype == VP_BF16 ? 8 : 4;
+  const int64_t kv = static_cast<int64_t>(s->n_kv_heads) * s->head_dim, qw = static_cast<int64_t>(s->n_q_heads) * s->head_dim;
+  if (t->k_stride < kv || t->v_stride < kv || (t->q && t->q_stride < qw))
+    return fail(VP_ERR_SHAPE, "a token's rows overlap the next one's (q_stride %lld, k_stride %lld, v_stride %lld)",
+                (long long)t->q_stride, (long long)t->k_stride, (long long)t->v_stride);
+  if (t->k_stride % step || t->v_stride % step || (t->q && t->q_stride % step))
+    return fail(VP_ERR_SHAPE, "token strides must be multiples of %lld elements (16 bytes)", (long long)step);
+  if (t->q && t->q == q_out && t->q_stride != qw) return fail(VP_ERR_SHAPE, "q_out is q, whose tokens are not next to each other");
+  if (reinterpret_cast<uintptr_t>(t->new_off) & 3u) return fail(VP_ERR_SHAPE, "new_off must be 4-byte aligned");
+  if (t->n_tokens < 0 || t->n_tokens > kMaxTokens) return fail(VP_ERR_RANGE, "n_tokens %d outside [0, %d]", t->n_tokens, kMaxTokens);
+  if (!t->new_off && t->n_tokens != static_cast<int64_t>(s->batch) * queries(*s))
+    return fail(VP_ERR_SHAPE, "n_tokens %d without new_off: batch %d x n_queries %d", t->n_tokens, s->batch, queries(*s));
+  return VP_OK;
+}
+
+// written: the caller's buffers are filled, so the heads' rows must not overlap
+vp_status check_kv4(const vp_shape* s, const vp_kv4* c, bool written) {
+  if (!c) return fail(VP_ERR_NULL, "cache is NULL");
+  if (!c->k_codes || !c->k_scales || !c->v_codes || !c->v_scales)
+    return fail(VP_ERR_NULL, "k_codes, k_scales, v_codes, v_scales required");
+  if (!aligned16(c->k_codes) || !aligned16(c->k_scales) || !aligned16(c->v_codes) || !aligned16(c->v_scales))
+    return fail(VP_ERR_SHAPE, "codes and scales must be 16-byte aligned");
+  if (s->block_size > 0 && s->block_size < 16)
+    return fail(VP_ERR_UNSUPPORTED, "block_size %d: blocks of 4-bit caches hold 16 rows or more", s->block_size);
+  if (c->code_stride_b < 0 || c->code_stride_h < 0 || c->scale_stride_b < 0 || c->scale_stride_h < 0)
+    return fail(VP_ERR_SHAPE, "negative 4-bit cache stride");
+  if (c->code_stride_b % 16 || c->code_stride_h % 16 || c->scale_stride_b % 16 || c->scale_stride_h % 16)
+    return fail(VP_ERR_SHAPE, "strides of 4-bit caches must be multiples of 16 bytes");
+  if (!written) return VP_OK;
+  if (c->k_codes == c->v_codes || c->k_scales == c->v_scales) return fail(VP_ERR_SHAPE, "K and V are the same cache");
+  const int64_t rows = s->block_size > 0 ? s->block_size : s->max_seq_len;
+  const int64_t count_b = s->block_size > 0 ? 2 : s->batch;  // (blocks: any two)
+  auto apart = [&](int64_t sb, int64_t sh, int64_t row_bytes) {
+    int64_t small = sh, n = s->n_kv_heads, large = sb, m = count_b;
+    if (sb < sh) std::swap(small, large), std::swap(n, m);
+    int64_t span = rows * row_bytes;
+    if (n > 1 && small < span) return false;
+    if (n > 1) span += small * (n - 1);
+    return m < 2 || large >= span;
+  };
+  if (!apart(c->code_stride_b, c->code_stride_h, s->head_dim / 2) || !apart(c->scale_stride_b, c->scale_stride_h, s->head_dim / 32))
+    return fail(VP_ERR_SHAPE, "rows of the 4-bit cache overlap");
+  return VP_OK;
+}
+
+Kv4Cache kv4_of(const vp_kv4* c) {
+  return {static_cast<uint8_t*>(c->k_codes), static_cast<uint8_t*>(c->k_scales), static_cast<uint8_t*>(c->v_codes),
+          static_cast<uint8_t*>(c->v_scales), c->code_stride_b, c->code_stride_h, c->scale_stride_b, c->scale_stride_h};
+}
+
+// What the two appending calls have in common
+AppendArgs append_args(const vp_shape* s, const vp_layout* layout, const vp_rope* rope, const vp_tokens* t, void* q_out) {
+  const int64_t esz = s->dtype == VP_BF16 ? 2 : 4;
+  AppendArgs a{};
+  a.q = t->q;
+  a.k = t->k;
+  a.v = t->v;
+  a.q_out = q_out;
+  a.qs = t->q_stride * esz;
+  a.ks = t->k_stride * esz;
+  a.vs = t->v_stride * esz;
+  if (s->block_size > 0) {
+    a.bs_log2 = __builtin_ctz(static_cast<unsigned>(s->block_size));
+    a.nblk = (s->max_seq_len + s->block_size - 1) / s->block_size;
+    a.block_table = layout->block_table;
+  }
+  a.seq_len = layout->seq_len;
+  a.new_off = t->new_off;
+  a.B = s->batch;
+  a.Hq = s->n_q_heads;
+  a.Hkv = s->n_kv_heads;
+  a.T = queries(*s);
+  a.max_seq_len = s->max_seq_len;
+  a.n_tokens = t->n_tokens;
+  if (rope) {
+    a.cos_sin = rope->cos_sin;
+    a.pos = rope->pos;
+    a.n_pos = rope->n_pos;
+    a.rot = rope->rot_dim;
+    a.interleaved = rope->interleaved;
+    a.axes = rope->n_axes;
+    int end = 0;
+    for (int i = 0; i < kMaxAxes; ++i) a.section_end[i] = end += i < rope->n_axes ? rope->section[i] : 0;
+  }
+  return a;
 }
 
 // Host checks of a whole decode step's arguments (everything but the workspace).
@@ -747,44 +902,13 @@ vp_status vp_window_decode_attn(const vp_shape* shape, const vp_layout* layout, 
   if (reinterpret_cast<uintptr_t>(attn_sum) & 3u) return fail(VP_ERR_SHAPE, "attn_sum must be 4-byte aligned");
   const WindowPlan plan = make_window_plan(*shape, *window, attn_sum != nullptr);
   if (vp_status e = check_room(workspace, workspace_bytes, plan.total)) return e;
-  char* ws = static_cast<char*>(workspace);
-  WindowArgs a{};
-  a.q = q;
+  WindowArgs a = window_args(shape, layout, window, plan, static_cast<char*>(workspace), q, out);
   a.K = K;
   a.V = V;
-  a.out = out;
   a.attn_sum = attn_sum;
   a.sb = shape->kv_stride_b;
   a.sh = shape->kv_stride_h;
   a.ss = shape->kv_stride_s;
-  a.bs_log2 = -1;
-  if (shape->block_size > 0) {
-    a.bs_log2 = __builtin_ctz(static_cast<unsigned>(shape->block_size));
-    a.nblk = (shape->max_seq_len + shape->block_size - 1) / shape->block_size;
-    a.block_table = layout->block_table;
-  }
-  a.seq_len = layout->seq_len;
-  a.B = shape->batch;
-  a.Hq = shape->n_q_heads;
-  a.Hkv = shape->n_kv_heads;
-  a.G = shape->n_q_heads / shape->n_kv_heads;
-  a.T = queries(*shape);
-  a.max_seq_len = shape->max_seq_len;
-  a.window = std::min(window->window, 2 * kMaxTokens);  // (further back than any row)
-  a.n_sink = window->n_sink;
-  const float sm = window->sm_scale > 0.f ? window->sm_scale : 1.0f / std::sqrt(static_cast<float>(shape->head_dim));
-  // log2(e); the largest scales stay finite, as an infinite one makes a NaN of the maximum's weight
-  a.zscale = std::min(sm * 1.4426950408889634f, 0x1.fffffep127f);
-  // weights stay below 2^8, and rescaling is rare; small beside the maximum that precedes
-  // the first row (-FLT_MAX), which every product exceeds
-  a.raise = std::min(8.f / a.zscale, 0x1p100f);
-  a.tiles = plan.tiles;
-  a.groups = plan.groups;
-  a.gp = plan.gp;
-  a.stats = reinterpret_cast<float*>(ws + plan.stats);
-  a.acc = reinterpret_cast<float*>(ws + plan.acc);
-  a.pieces = reinterpret_cast<int2*>(ws + plan.pieces);
-  a.zs = reinterpret_cast<float*>(ws + plan.zs);
   if (hipError_t e = launch_window(a, shape->dtype, shape->head_dim, static_cast<hipStream_t>(stream)))
     return hip_fail(e, "window attention launch");
   return VP_OK;
@@ -851,6 +975,104 @@ vp_status vp_evict(const vp_shape* shape, const vp_layout* layout, const vp_evic
   a.turn_words = plan.turn_words;
   if (hipError_t e = launch_evict(a, static_cast<int>(shape->head_dim * esz), static_cast<hipStream_t>(stream)))
     return hip_fail(e, "eviction launch");
+  return VP_OK;
+}
+
+vp_status vp_append_kv(const vp_shape* shape, const vp_layout* layout, const vp_rope* rope, const vp_tokens* tokens,
+                       void* q_out, void* K, void* V, void* stream) {
+  g_last_error.clear();
+  if (vp_status e = check_shape(shape)) return e;
+  if (vp_status e = check_rows(shape, layout)) return e;
+  if (vp_status e = check_rope(shape, rope)) return e;
+  if (vp_status e = check_tokens(shape, tokens, q_out)) return e;
+  if (!K || !V) return fail(VP_ERR_NULL, "K, V required");
+  if (!aligned16(K) || !aligned16(V)) return fail(VP_ERR_SHAPE, "K, V must be 16-byte aligned");
+  if (vp_status e = check_rows_apart(shape)) return e;
+  if (K == V) return fail(VP_ERR_SHAPE, "K and V are the same cache");
+  const int64_t esz = shape->dtype == VP_BF16 ? 2 : 4;
+  AppendArgs a = append_args(shape, layout, rope, tokens, q_out);
+  a.K = K;
+  a.V = V;
+  a.sb = shape->kv_stride_b * esz;
+  a.sh = shape->kv_stride_h * esz;
+  a.ss = shape->kv_stride_s * esz;
+  if (hipError_t e = launch_append(a, false, shape->dtype, shape->head_dim, static_cast<hipStream_t>(stream)))
+    return hip_fail(e, "append launch");
+  return VP_OK;
+}
+
+vp_status vp_append_kv4(const vp_shape* shape, const vp_layout* layout, const vp_rope* rope, const vp_tokens* tokens,
+                        void* q_out, const vp_kv4* cache, void* stream) {
+  g_last_error.clear();
+  if (vp_status e = check_shape(shape)) return e;
+  if (vp_status e = check_rows(shape, layout)) return e;
+  if (vp_status e = check_rope(shape, rope)) return e;
+  if (vp_status e = check_tokens(shape, tokens, q_out)) return e;
+  if (vp_status e = check_kv4(shape, cache, true)) return e;
+  AppendArgs a = append_args(shape, layout, rope, tokens, q_out);
+  a.four = kv4_of(cache);
+  if (hipError_t e = launch_append(a, true, shape->dtype, shape->head_dim, static_cast<hipStream_t>(stream)))
+    return hip_fail(e, "4-bit append launch");
+  return VP_OK;
+}
+
+vp_status vp_kv4_read(const vp_shape* shape, const vp_layout* layout, const vp_kv4* cache, const int32_t* first, void* K,
+                      void* V, void* stream) {
+  g_last_error.clear();
+  if (vp_status e = check_shape(shape)) return e;
+  if (vp_status e = check_rows(shape, layout)) return e;
+  if (vp_status e = check_kv4(shape, cache, false)) return e;
+  if (!K || !V) return fail(VP_ERR_NULL, "K, V required");
+  if (!aligned16(K) || !aligned16(V)) return fail(VP_ERR_SHAPE, "K, V must be 16-byte aligned");
+  if (vp_status e = check_rows_apart(shape)) return e;
+  if (K == V) return fail(VP_ERR_SHAPE, "K and V are the same cache");
+  if (reinterpret_cast<uintptr_t>(first) & 3u) return fail(VP_ERR_SHAPE, "first must be 4-byte aligned");
+  const int64_t esz = shape->dtype == VP_BF16 ? 2 : 4;
+  ReadArgs a{};
+  a.four = kv4_of(cache);
+  a.K = K;
+  a.V = V;
+  a.sb = shape->kv_stride_b * esz;
+  a.sh = shape->kv_stride_h * esz;
+  a.ss = shape->kv_stride_s * esz;
+  if (shape->block_size > 0) {
+    a.bs_log2 = __builtin_ctz(static_cast<unsigned>(shape->block_size));
+    a.nblk = (shape->max_seq_len + shape->block_size - 1) / shape->block_size;
+    a.block_table = layout->block_table;
+  }
+  a.seq_len = layout->seq_len;
+  a.first = first;
+  a.B = shape->batch;
+  a.Hkv = shape->n_kv_heads;
+  a.max_seq_len = shape->max_seq_len;
+  if (hipError_t e = launch_kv4_read(a, shape->dtype, shape->head_dim, static_cast<hipStream_t>(stream)))
+    return hip_fail(e, "4-bit read launch");
+  return VP_OK;
+}
+
+vp_status vp_kv4_workspace_size(const vp_shape* shape, const vp_window* window, size_t* bytes) {
+  g_last_error.clear();
+  if (vp_status e = check_shape(shape)) return e;
+  if (vp_status e = check_window(window)) return e;
+  if (!bytes) return fail(VP_ERR_NULL, "bytes is NULL");
+  *bytes = make_kv4_plan(*shape, *window).total;
+  return VP_OK;
+}
+
+vp_status vp_kv4_decode_attn(const vp_shape* shape, const vp_layout* layout, const vp_window* window, const void* q,
+                             const vp_kv4* cache, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  g_last_error.clear();
+  if (vp_status e = check_shape(shape)) return e;
+  if (vp_status e = check_rows(shape, layout)) return e;
+  if (vp_status e = check_window(window)) return e;
+  if (vp_status e = check_kv4(shape, cache, false)) return e;
+  if (!q || !out) return fail(VP_ERR_NULL, "q, out required");
+  if (!aligned16(q) || !aligned16(out)) return fail(VP_ERR_SHAPE, "q, out must be 16-byte aligned");
+  const WindowPlan plan = make_kv4_plan(*shape, *window);
+  if (vp_status e = check_room(workspace, workspace_bytes, plan.total)) return e;
+  const WindowArgs a = window_args(shape, layout, window, plan, static_cast<char*>(workspace), q, out);
+  if (hipError_t e = launch_kv4_attention(a, kv4_of(cache), shape->dtype, shape->head_dim, static_cast<hipStream_t>(stream)))
+    return hip_fail(e, "4-bit attention launch");
   return VP_OK;
 }
 

@@ -45,6 +45,12 @@ struct WindowArgs {
 };
 hipError_t launch_window(const WindowArgs& a, int dtype, int head_dim, hipStream_t st);
 
+// Pieces of the above that attention over 4-bit caches shares: the tiles of the longest walk,
+// the workspace's parts for a plan of so many work-groups, and the launch that joins the pieces.
+int window_tiles(const vp_shape& s, const vp_window& w);
+void carve_window_plan(WindowPlan& p, const vp_shape& s, bool sums);
+hipError_t launch_window_join(const WindowArgs& a, int dtype, int head_dim, hipStream_t st);
+
 // The rows that the queries of one sequence see, as a walk over 32-row tiles of
 // positions: the tiles of the first n_sink rows, then those of the window. Query t is
 // the token at position L - T + t and sees the positions j <= L - T + t with j < n_sink

@@ -48,22 +48,13 @@
 #include "vp_blocks.h"
 #include "vp_cache.h"
 #include "vp_tile.h"
+#include "vp_walk.h"
 
 namespace vp {
 namespace {
 
-constexpr int kWinWaves = 4;
-constexpr int kWinThreads = 64 * kWinWaves;
-
 // s_waitcnt operand: at most n vector memory operations left (n < 64), others unconstrained
 constexpr int wait_vm(int n) { return kWaitVm0 | (n & 15) | (n >> 4) << 14; }
-
-size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
-
-// 2^(c (z - m)) of products z and m, m at most a.raise below z: the difference first, so
-// that the weight of the largest product is what it should be however large it is (in one
-// fma, with m scaled and rounded, it is off by 2^(c m 2^-25): from 2^31 on out of range)
-__device__ __forceinline__ float weight_of(const WindowArgs& a, float z, float m) { return fast_exp2((z - m) * a.zscale); }
 
 template <int DT, int D, bool SUMS>
 struct WinLds {
@@ -73,111 +64,6 @@ struct WinLds {
   static constexpr int K_BYTES = C::SUB_ROWS_BYTES > 16 * PITCH * 4 ? C::SUB_ROWS_BYTES : 16 * PITCH * 4;
   static constexpr int V_BYTES = C::SUB_ROWS_BYTES;
   static constexpr int STAGE_BYTES = SUMS ? C::STAGE_BYTES : 16;
-};
-
-// (max, sum) of the query rows, per wave
-struct WinStats {
-  float m[kWinWaves][16];
-  float l[kWinWaves][16];
-};
-
-template <int DT>
-__device__ __forceinline__ void store_out(void* out, size_t row, int D, int col4, float4 v) {
-  if constexpr (DT == VP_BF16) {
-    uint2 o;
-    o.x = f32_to_bf16_bits(v.x) | (static_cast<uint32_t>(f32_to_bf16_bits(v.y)) << 16);
-    o.y = f32_to_bf16_bits(v.z) | (static_cast<uint32_t>(f32_to_bf16_bits(v.w)) << 16);
-    reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + row * D)[col4] = o;
-  } else {
-    reinterpret_cast<float4*>(static_cast<float*>(out) + row * D)[col4] = v;
-  }
-}
-
-// row of out [B][T][Hq] for query row r (query t = r / G, head g*G + r % G)
-__device__ __forceinline__ size_t out_row(const WindowArgs& a, int b, int g, int r) {
-  return (static_cast<size_t>(b) * a.T + r / a.G) * a.Hq + g * a.G + r % a.G;
-}
-
-__device__ __forceinline__ WindowWalk walk_of(const WindowArgs& a, int b) {
-  return WindowWalk(clamp_len(a.seq_len[b], a.max_seq_len), a.T, a.window, a.n_sink);
-}
-
-// How the walks of a batch are dealt to `groups` work-groups, found by every wave from
-// the lengths (no barrier): a work-group takes about `share` tiles of one pair, so a pair
-// of n tiles has ceil(n / share) of them, its parts. Up to 64 sequences have a lane each,
-// one load of the lengths is all that is read, and share is about the least whose
-// work-groups are not too many; more sequences have consecutive ones in every lane, and
-// share is what always fits.
-struct Deal {
-  int b, g, part, parts;  // this work-group's sequence, KV head and part of parts; b < 0: none
-  int L;                  // the sequence's length
-  __device__ __forceinline__ Deal(const WindowArgs& a, int lane, int group) {
-    const int per = (a.B + 63) / 64;
-    const int i0 = lane * per, i1 = min(a.B, i0 + per);
-    int len = 0, mine = 0;  // of a lane's sequences: the (one) length, their tiles
-    if (per == 1) {
-      len = i0 < i1 ? clamp_len(a.seq_len[i0], a.max_seq_len) : 0;
-      mine = tiles(a, len);
-    } else {
-      mine = sum(a, i0, i1, [](int n) { return n; });
-    }
-    const int total = a.Hkv * __builtin_amdgcn_readlane(wave_incl_sum(mine), 63);
-    const int pairs = a.Hkv * a.B;
-    int share = (total + a.groups - 1) / a.groups, count = 0;
-    share = max(share, kWinWaves);  // a tile per wave at least
-    if (per == 1) {
-      // (ends: a share of the longest walk gives every pair one part, and there are as many groups)
-      for (;; share += max(1, share / 32)) {
-        count = wave_incl_sum(split(mine, share));
-        if (a.Hkv * __builtin_amdgcn_readlane(count, 63) <= a.groups) break;
-      }
-      mine = split(mine, share);
-    } else {
-      share = max(share, (total + a.groups - pairs - 1) / (a.groups - pairs));
-      mine = sum(a, i0, i1, [&](int n) { return split(n, share); });
-      count = wave_incl_sum(mine);
-    }
-    // count: parts of this lane's sequences and those before, for one KV head
-    const bool here = a.Hkv * (count - mine) <= group && group < a.Hkv * count;
-    const uint64_t found = __builtin_amdgcn_ballot_w64(here);
-    b = -1;
-    if (found == 0) return;
-    const int src = __builtin_ctzll(found);
-    int before = count - mine, at = i0, own = mine;
-    if (per > 1 && here) {
-      for (own = split(walk_of(a, at).n, share); group >= a.Hkv * (before + own); own = split(walk_of(a, at).n, share)) {
-        before += own;
-        ++at;
-      }
-    }
-    b = __builtin_amdgcn_readlane(at, src);
-    parts = __builtin_amdgcn_readlane(own, src);
-    const int i = group - a.Hkv * __builtin_amdgcn_readlane(before, src);
-    g = i / parts;
-    part = i - g * parts;
-    L = per == 1 ? __builtin_amdgcn_readlane(len, src) : clamp_len(a.seq_len[b], a.max_seq_len);
-  }
-
- private:
-  static __device__ __forceinline__ int tiles(const WindowArgs& a, int len) {
-    return WindowWalk(len, a.T, a.window, a.n_sink).n;
-  }
-  static __device__ __forceinline__ int split(int n, int share) {
-    return static_cast<int>((static_cast<unsigned>(n) + share - 1) / static_cast<unsigned>(share));
-  }
-  // f(tiles) over sequences i0 .. i1 - 1, four loads in flight
-  template <typename F>
-  static __device__ __forceinline__ int sum(const WindowArgs& a, int i0, int i1, F f) {
-    int s = 0;
-    for (int i = i0; i < i1; i += 4) {
-      int n[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) n[j] = walk_of(a, min(i + j, a.B - 1)).n;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) s += i + j < i1 ? f(n[j]) : 0;
-    }
-    return s;
-  }
 };
 
 // Scores of half a tile. fp32: four sums of a quarter of the products each, added in
@@ -716,24 +602,35 @@ hipError_t launch_dd(const WindowArgs& a, hipStream_t st) {
   else hipLaunchKernelGGL((window_kernel<DT, D, false, false>), grid, dim3(kWinThreads), 0, st, a);
   if (hipError_t e = hipGetLastError()) return e;
   if (a.groups == 0) return hipSuccess;
-  const int heads = a.T * a.G;
   // (a capacity far above the lengths costs no more work-groups than a full GPU needs)
   const int64_t pairs = static_cast<int64_t>(a.B) * a.Hkv;
   const int64_t most = std::max<int64_t>(1, 8192 / pairs);
   const int rows = sums ? static_cast<int>(std::min<int64_t>(most, (a.tiles * 32ll + kFinishThreads - 1) / kFinishThreads)) : 0;
+  const int heads = a.T * a.G;
   hipLaunchKernelGGL((finish_kernel<DT, D>), dim3(heads + rows, a.Hkv, a.B), dim3(kFinishThreads), 0, st, a, heads);
+  return hipGetLastError();
+}
+
+template <int DT, int D>
+hipError_t join_dd(const WindowArgs& a, hipStream_t st) {
+  const int heads = a.T * a.G;
+  hipLaunchKernelGGL((finish_kernel<DT, D>), dim3(heads, a.Hkv, a.B), dim3(kFinishThreads), 0, st, a, heads);
   return hipGetLastError();
 }
 
 }  // namespace
 
+int window_tiles(const vp_shape& s, const vp_window& w) {
+  const int64_t T = queries(s), cap = (static_cast<int64_t>(s.max_seq_len) + 31) / 32;
+  if (w.window == 0) return static_cast<int>(cap);
+  // the window's rows may begin anywhere in a tile
+  return static_cast<int>(std::min(cap, (static_cast<int64_t>(w.n_sink) + 31) / 32 + (w.window + T - 1 + 30) / 32 + 1));
+}
+
 WindowPlan make_window_plan(const vp_shape& s, const vp_window& w, bool sums) {
   WindowPlan p{};
-  const int64_t T = queries(s), cap = (static_cast<int64_t>(s.max_seq_len) + 31) / 32;
-  int64_t tiles = cap;
-  if (w.window > 0)  // the window's rows may begin anywhere in a tile
-    tiles = std::min(cap, (static_cast<int64_t>(w.n_sink) + 31) / 32 + (w.window + T - 1 + 30) / 32 + 1);
-  p.tiles = static_cast<int>(tiles);
+  const int64_t cap = (static_cast<int64_t>(s.max_seq_len) + 31) / 32;
+  const int64_t tiles = p.tiles = window_tiles(s, w);
   const int64_t pairs = static_cast<int64_t>(s.batch) * s.n_kv_heads;
   // One work-group per pair, and no second launch, where
   // * the walks are short: up to 16 tiles, 12 with sums (bf16; 8 KV heads of 128, 16 tiles:
@@ -768,7 +665,13 @@ WindowPlan make_window_plan(const vp_shape& s, const vp_window& w, bool sums) {
   // times as many 53.1)
   const int64_t most = std::max<int64_t>(resident_groups(s.dtype, s.head_dim), 2 * pairs);
   p.groups = one_each ? 0 : static_cast<int>(std::min(most, pairs * ((tiles + kWinWaves - 1) / kWinWaves)));
-  const int rows = static_cast<int>(T) * (s.n_q_heads / s.n_kv_heads);
+  carve_window_plan(p, s, sums);
+  return p;
+}
+
+void carve_window_plan(WindowPlan& p, const vp_shape& s, bool sums) {
+  const int64_t pairs = static_cast<int64_t>(s.batch) * s.n_kv_heads;
+  const int rows = queries(s) * (s.n_q_heads / s.n_kv_heads);
   p.gp = 1;
   while (p.gp < rows) p.gp *= 2;
   const size_t pieces = p.groups;
@@ -782,7 +685,6 @@ WindowPlan make_window_plan(const vp_shape& s, const vp_window& w, bool sums) {
   p.zs = off;
   if (sums) off = align256(off + static_cast<size_t>(pairs) * p.tiles * 32 * p.gp * 4);
   p.total = off;
-  return p;
 }
 
 hipError_t launch_window(const WindowArgs& a, int dtype, int head_dim, hipStream_t st) {
@@ -794,6 +696,11 @@ hipError_t launch_window(const WindowArgs& a, int dtype, int head_dim, hipStream
     if (head_dim == 64) return launch_dd<VP_F32, 64>(a, st);
   }
   return hipErrorInvalidValue;
+}
+
+hipError_t launch_window_join(const WindowArgs& a, int dtype, int head_dim, hipStream_t st) {
+  if (dtype == VP_BF16) return head_dim == 128 ? join_dd<VP_BF16, 128>(a, st) : join_dd<VP_BF16, 64>(a, st);
+  return head_dim == 128 ? join_dd<VP_F32, 128>(a, st) : join_dd<VP_F32, 64>(a, st);
 }
 
 }  // namespace vp

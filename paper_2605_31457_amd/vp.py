@@ -55,6 +55,24 @@ class vp_evict_params(ctypes.Structure):
     _fields_ = [("budget", ctypes.c_int32), ("n_sink", ctypes.c_int32), ("n_recent", ctypes.c_int32)]
 
 
+class vp_rope(ctypes.Structure):
+    _fields_ = [("cos_sin", ctypes.c_void_p), ("n_pos", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("pos", ctypes.c_void_p),
+                ("section", ctypes.c_int32 * 4)]
+
+
+class vp_tokens(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("new_off", ctypes.c_void_p),
+                ("n_tokens", ctypes.c_int32)]
+
+
+class vp_kv4(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("code_stride_b", ctypes.c_int64), ("code_stride_h", ctypes.c_int64),
+                ("scale_stride_b", ctypes.c_int64), ("scale_stride_h", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -87,6 +105,11 @@ def lib() -> ctypes.CDLL:
             "vp_window_decode_attn": ([P(vp_shape), P(vp_layout), P(vp_window), V, V, V, V, V, V, S, V], ctypes.c_int),
             "vp_evict_workspace_size": ([P(vp_shape), P(vp_evict_params), P(S)], ctypes.c_int),
             "vp_evict": ([P(vp_shape), P(vp_layout), P(vp_evict_params), V, V, V, V, V, V, V, V, S, V], ctypes.c_int),
+            "vp_append_kv": ([P(vp_shape), P(vp_layout), P(vp_rope), P(vp_tokens), V, V, V, V], ctypes.c_int),
+            "vp_append_kv4": ([P(vp_shape), P(vp_layout), P(vp_rope), P(vp_tokens), V, P(vp_kv4), V], ctypes.c_int),
+            "vp_kv4_read": ([P(vp_shape), P(vp_layout), P(vp_kv4), V, V, V, V], ctypes.c_int),
+            "vp_kv4_workspace_size": ([P(vp_shape), P(vp_window), P(S)], ctypes.c_int),
+            "vp_kv4_decode_attn": ([P(vp_shape), P(vp_layout), P(vp_window), V, P(vp_kv4), V, V, S, V], ctypes.c_int),
             "vp_stream_read": ([V, S, ctypes.c_int32, V, V], ctypes.c_int),
             "vp_decode_step_static": ([P(vp_shape), P(vp_layout), P(vp_params), V, V, V, V, V, V, V, V, V, V],
                                        ctypes.c_int),
@@ -280,6 +303,49 @@ def vp_evict(shape, layout, params, attn_sum, K, V, kept, attn_sum_out, vis_seg_
     _check("vp_evict", lib().vp_evict(
         ctypes.byref(shape), ctypes.byref(layout), ctypes.byref(params), _p(attn_sum), _p(K), _p(V), _p(kept),
         _p(attn_sum_out), _p(vis_seg_out), _p(new_len), _p(workspace), nbytes, _stream(stream)))
+
+
+def _ref(struct):
+    return None if struct is None else ctypes.byref(struct)
+
+
+def vp_append_kv(shape, layout, rope, tokens, q_out, K, V, stream=None):
+    """New tokens (vp_tokens) to the last rows of their sequences, queries and keys rotated
+    (rope None: as they are); q_out None without queries."""
+    _on_current_device("vp_append_kv", q_out, K, V)
+    _check("vp_append_kv", lib().vp_append_kv(
+        ctypes.byref(shape), ctypes.byref(layout), _ref(rope), ctypes.byref(tokens), _p(q_out), _p(K), _p(V),
+        _stream(stream)))
+
+
+def vp_append_kv4(shape, layout, rope, tokens, q_out, cache, stream=None):
+    """vp_append_kv into a 4-bit cache (vp_kv4)."""
+    _on_current_device("vp_append_kv4", q_out)
+    _check("vp_append_kv4", lib().vp_append_kv4(
+        ctypes.byref(shape), ctypes.byref(layout), _ref(rope), ctypes.byref(tokens), _p(q_out), ctypes.byref(cache),
+        _stream(stream)))
+
+
+def vp_kv4_read(shape, layout, cache, first, K, V, stream=None):
+    """Rows first[b] .. seq_len[b] - 1 (first None: all) of a 4-bit cache into K and V."""
+    _on_current_device("vp_kv4_read", first, K, V)
+    _check("vp_kv4_read", lib().vp_kv4_read(
+        ctypes.byref(shape), ctypes.byref(layout), ctypes.byref(cache), _p(first), _p(K), _p(V), _stream(stream)))
+
+
+def vp_kv4_workspace_size(shape: vp_shape, window: vp_window) -> int:
+    n = ctypes.c_size_t(0)
+    _check("vp_kv4_workspace_size", lib().vp_kv4_workspace_size(ctypes.byref(shape), ctypes.byref(window), ctypes.byref(n)))
+    return n.value
+
+
+def vp_kv4_decode_attn(shape, layout, window, q, cache, out, workspace, workspace_bytes=None, stream=None):
+    """Attention over a window and the first tokens of a 4-bit cache."""
+    _on_current_device("vp_kv4_decode_attn", q, out, workspace)
+    nbytes = _room(workspace, workspace_bytes)
+    _check("vp_kv4_decode_attn", lib().vp_kv4_decode_attn(
+        ctypes.byref(shape), ctypes.byref(layout), ctypes.byref(window), _p(q), ctypes.byref(cache), _p(out),
+        _p(workspace), nbytes, _stream(stream)))
 
 
 def vp_validate_layout(shape, layout, stream=None):
