@@ -28,10 +28,9 @@ namespace {
 
 typedef __bf16 bf16x2 __attribute__((__vector_size__(2 * sizeof(__bf16))));
 
-// the scale byte as a float (the mark of a block that is all NaN: NaN)
-__device__ __forceinline__ float scale_of(uint32_t byte) {
-  return __uint_as_float(byte == kScaleNan ? 0x7fc00000u : byte << 23);
-}
+// The conversions take a scale's exponent bits alone (23 to 30; sign and mantissa do not
+// count; 0 is 2^-127, 255 makes NaN).
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 // elements 2 B and 2 B + 1 of 8 codes, times the scale, as two bf16
 template <int B>
@@ -81,8 +80,7 @@ __global__ __launch_bounds__(kReadThreads) void read_kernel(const ReadArgs a) {
     for (int j = 0; j < BATCH; ++j) {
       if (r0 + j * ROWS + static_cast<int>(threadIdx.x) / LANES >= L) continue;
       const float scale = scale_of(s[j]);
-      uint32_t w[4] = {two_of<0>(c[j], scale), two_of<1>(c[j], scale), two_of<2>(c[j], scale), two_of<3>(c[j], scale)};
-      if (s[j] == kScaleNan) w[0] = w[1] = w[2] = w[3] = 0x7fc07fc0u;
+      const uint32_t w[4] = {two_of<0>(c[j], scale), two_of<1>(c[j], scale), two_of<2>(c[j], scale), two_of<3>(c[j], scale)};
       char* dst = out + at[j] * a.sb + in[j] * a.ss;
       if constexpr (DT == VP_BF16) {
         *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -167,19 +165,27 @@ struct Queries {
 // what a lane holds of a tile of 32 rows
 template <int D>
 struct Tile {
-  static constexpr int KW = D / 32;          // dwords of a key row's piece, its dims (D/4) a4 ..
-  uint32_t k[2][KW];                         // rows 16 half + n16
-  uint32_t ks[2];                            // their scale bytes
-  uint32_t v[8];                             // rows pv_token(a4, i): elements (D/16) n16 ..
-  uint32_t vs[8];                            // their scale bytes
+  static constexpr int KW = D / 32;  // dwords of a key row's piece, its dims (D/4) a4 ..
+  static constexpr int VS = D / 16;  // dwords of the value rows' scales
+  uint32_t k[2][KW];                 // rows 16 half + n16
+  uint32_t ks[2];                    // their scale bytes
+  uint32_t v[8];                     // rows pv_token(a4, i): elements (D/16) n16 ..
+  uint32_t vs[VS];                   // all their scales: row i in dword i (D = 128), in half i % 2 of dword i / 2
 };
 
+// A value row's scale: a lane's elements lie in one block of 32, whose byte comes to bits 23 to 30
+template <int D>
+__device__ __forceinline__ uint32_t value_scale(const Tile<D>& t, int i, int n16) {
+  if constexpr (D == 128) return __builtin_amdgcn_alignbit(t.vs[i], t.vs[i], (8 * (n16 >> 2) + 9) & 31);
+  else return __builtin_amdgcn_alignbit(t.vs[i >> 1], t.vs[i >> 1], (8 * (n16 >> 3) + 16 * (i & 1) + 9) & 31);
+}
+
 template <int D, int N>
-__device__ __forceinline__ void scores(f32x4 (&c)[2], const Tile<D>& t, const bf16x8 (&q)[N][D / 32]) {
+__device__ __forceinline__ void scores(float (&z)[8], const Tile<D>& t, const bf16x8 (&q)[N][D / 32]) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const float scale = scale_of(t.ks[h]);
-    c[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+    f32x4 c = {0.f, 0.f, 0.f, 0.f};
     bf16x8 k[D / 32];
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) {
@@ -189,75 +195,175 @@ __device__ __forceinline__ void scores(f32x4 (&c)[2], const Tile<D>& t, const bf
 #pragma unroll
     for (int p = N - 1; p >= 0; --p)
 #pragma unroll
-      for (int s = 0; s < D / 32; ++s) c[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[s], q[p][s], c[h], 0, 0, 0);
+      for (int s = 0; s < D / 32; ++s) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[s], q[p][s], c, 0, 0, 0);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) z[4 * h + r] = c[r];
   }
 }
 
-// acc[e][r] (dim (D/16) (4 a4 + r) + e of head n16) += V^T P^T over the tile's 32 rows. The
-// weights enter as the sum of three bf16 numbers, all 24 bits of them.
-template <int D>
-__device__ __forceinline__ void values(f32x4 (&acc)[D / 16], const Tile<D>& t, const float (&p)[8]) {
-  uint32_t pf[4], pm[4], pl[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    uint32_t a[2], b[2], c[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      a[i] = __float_as_uint(p[2 * j + i]);
-      const float r = p[2 * j + i] - __uint_as_float(a[i] & 0xffff0000u);
-      b[i] = __float_as_uint(r);
-      c[i] = __float_as_uint(r - __uint_as_float(b[i] & 0xffff0000u));
-    }
-    // the leading halves of two floats as a pair
-    pf[j] = __builtin_amdgcn_perm(a[1], a[0], 0x07060302u);
-    pm[j] = __builtin_amdgcn_perm(b[1], b[0], 0x07060302u);
-    pl[j] = __builtin_amdgcn_perm(c[1], c[0], 0x07060302u);  // (at most 8 bits: exact)
+// The value product. The weights enter as the sum of three bf16 numbers, all 24 bits of
+// them (truncated one after another: exact).
+//
+// FOLD, up to 8 query rows: a matrix product's 16 columns are 8 query rows for the elements
+// of even number and the same 8 for those of odd number, and its 32 slots are 16 rows of V times
+// the two elements of a code byte: the weights of the other parity are zeros. So a
+// byte's conversion is an operand as it stands, nothing is sorted, and the accumulators have
+// no idle columns. acc[byte][r]: element (D/16) (4 a4 + r) + 2 byte + (n16 >> 3) of query row n16 & 7.
+// Else: acc[e][r]: element (D/16) (4 a4 + r) + e of query row n16, slots are 32 rows of V, and
+// pairs of conversions are sorted by element.
+template <int D, bool FOLD>
+struct Values {
+  static constexpr int N = FOLD ? D / 32 : D / 16;
+  f32x4 acc[N];
+
+  __device__ __forceinline__ static float rest(float p) {
+    return p - __uint_as_float(__float_as_uint(p) & 0xffff0000u);
   }
-  const bf16x8 w0 = __builtin_bit_cast(bf16x8, make_uint4(pf[0], pf[1], pf[2], pf[3]));
-  const bf16x8 w1 = __builtin_bit_cast(bf16x8, make_uint4(pm[0], pm[1], pm[2], pm[3]));
-  const bf16x8 w2 = __builtin_bit_cast(bf16x8, make_uint4(pl[0], pl[1], pl[2], pl[3]));
-  float scale[8];
+  template <int B>
+  __device__ __forceinline__ void byte(const Tile<D>& t, const float (&scale)[8], const bf16x8 (&w)[FOLD ? 6 : 3]) {
+    if constexpr (FOLD) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) scale[i] = scale_of(t.vs[i]);
-  auto two_dims = [&](auto byte) {
-    constexpr int B = decltype(byte)::value;
-    uint32_t lo[4], hi[4];
+      for (int h = 0; h < 2; ++h) {
+        uint32_t x[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t x = two_of<B>(t.v[2 * j], scale[2 * j]), y = two_of<B>(t.v[2 * j + 1], scale[2 * j + 1]);
-      lo[j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-      hi[j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+        for (int j = 0; j < 4; ++j) x[j] = two_of<B>(t.v[4 * h + j], scale[4 * h + j]);
+        const bf16x8 a = __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
+#pragma unroll
+        for (int i = 0; i < 3; ++i) acc[B] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[3 * h + i], acc[B], 0, 0, 0);
+      }
+    } else {
+      uint32_t lo[4], hi[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t x = two_of<B>(t.v[2 * j], scale[2 * j]), y = two_of<B>(t.v[2 * j + 1], scale[2 * j + 1]);
+        lo[j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+        hi[j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+      }
+      const bf16x8 a0 = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+      const bf16x8 a1 = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        acc[2 * B] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, w[i], acc[2 * B], 0, 0, 0);
+        acc[2 * B + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, w[i], acc[2 * B + 1], 0, 0, 0);
+      }
     }
-    const bf16x8 a0 = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
-    const bf16x8 a1 = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-    acc[2 * B] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, w0, acc[2 * B], 0, 0, 0);
-    acc[2 * B + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, w0, acc[2 * B + 1], 0, 0, 0);
-    acc[2 * B] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, w1, acc[2 * B], 0, 0, 0);
-    acc[2 * B + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, w1, acc[2 * B + 1], 0, 0, 0);
-    acc[2 * B] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a0, w2, acc[2 * B], 0, 0, 0);
-    acc[2 * B + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a1, w2, acc[2 * B + 1], 0, 0, 0);
-  };
-  two_dims(std::integral_constant<int, 0>());
-  two_dims(std::integral_constant<int, 1>());
-  if constexpr (D == 128) {
-    two_dims(std::integral_constant<int, 2>());
-    two_dims(std::integral_constant<int, 3>());
   }
+  // p: the weights of rows pv_token(a4, i)
+  __device__ __forceinline__ void add(const Tile<D>& t, const float (&p)[8], int n16) {
+    bf16x8 w[FOLD ? 6 : 3];
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = p[i];
+    // a weight's upper half in the lower or the upper half of a dword
+    const uint32_t place = n16 < 8 ? 0x0c0c0302u : 0x03020c0cu;
+#pragma unroll
+    for (int part = 0; part < 3; ++part) {
+      uint32_t u[8];
+      if constexpr (FOLD) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = __builtin_amdgcn_perm(0u, __float_as_uint(x[i]), place);
+        w[part] = __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3]));
+        w[3 + part] = __builtin_bit_cast(bf16x8, make_uint4(u[4], u[5], u[6], u[7]));
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) u[j] = __builtin_amdgcn_perm(__float_as_uint(x[2 * j + 1]), __float_as_uint(x[2 * j]), 0x07060302u);
+        w[part] = __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3]));
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = rest(x[i]);
+    }
+    float scale[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) scale[i] = __uint_as_float(value_scale<D>(t, i, n16));
+    byte<0>(t, scale, w);
+    byte<1>(t, scale, w);
+    if constexpr (D == 128) {
+      byte<2>(t, scale, w);
+      byte<3>(t, scale, w);
+    }
+  }
+  // Tiles where some query does not see some row: blocks of NaN would reach the outputs of
+  // the queries that do not see them as 0 NaN. They are taken out of the tile (bit i of the
+  // result: this lane's block of row i is one), ...
+  __device__ __forceinline__ static unsigned take_nan(Tile<D>& t, int n16) {
+    unsigned bad = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bool b = (value_scale<D>(t, i, n16) & 0x7f800000u) == 0x7f800000u;
+      bad |= b ? 1u << i : 0u;
+      t.v[i] = b ? 0u : t.v[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      // (the lane's byte of that row's scales becomes 2^0; others are not this lane's to read)
+      const int at = D == 128 ? 8 * (n16 >> 2) : 8 * (n16 >> 3) + 16 * (i & 1);
+      uint32_t& s = t.vs[D == 128 ? i : i >> 1];
+      if ((bad >> i) & 1u) s = (s & ~(0xffu << at)) | 127u << at;
+    }
+    return bad;
+  }
+  // ... and the queries that do see one get NaN: by the number of such rows, a product of
+  // zeros and ones
+  __device__ __forceinline__ void put_nan(unsigned bad, unsigned seen) {
+    f32x4 count = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t x[4], y[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[j] = (bad >> (4 * h + j)) & 1u ? 0x3f803f80u : 0u;
+        y[j] = (seen >> (4 * h + j)) & 1u ? 0x3f803f80u : 0u;
+      }
+      count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3])),
+                                                      __builtin_bit_cast(bf16x8, make_uint4(y[0], y[1], y[2], y[3])), count, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[i][r] = count[r] > 0.f ? __builtin_nanf("") : acc[i][r];
+  }
+};
+
+// work-groups that a CU's registers hold (a wave of each per SIMD)
+constexpr int kv4_groups_per_cu(int dtype, int head_dim, bool fold) {
+  return (dtype == VP_F32 && head_dim == 128) || !fold ? 2 : 3;
 }
 
-template <int DT, int D, bool PAGED>
-__global__ __launch_bounds__(kWinThreads) void kv4_kernel(const WindowArgs a, const Kv4Cache four) {
+// The tiles of a walk all of whose rows every query sees, and the others, the outer ones: those at
+// the end of the sinks, at the beginning of the windows, and around the queries' own rows.
+struct Interior {
+  int a1;        // inner tiles 0 .. a1 - 1
+  int b0, b1;    // and b0 .. b1 - 1
+  int n, outer;  // how many inner and outer ones
+  __device__ __forceinline__ Interior(const WindowWalk& w, int T, int window) {
+    const int past = max(w.L - T + 1, 0);              // rows that lie before every query but the first's own, and that one
+    const int hidden = window > 0 ? w.L - window : 0;  // the last query sees no row from n_sink up to here
+    a1 = min(window > 0 ? w.S / 32 : w.sinks, past / 32);
+    b0 = max(w.sinks, w.sinks - w.first + (max(hidden, 0) + 31) / 32);
+    b0 = min(b0, w.n);
+    b1 = min(max(w.sinks - w.first + past / 32, b0), w.n);
+    n = a1 + (b1 - b0);
+    outer = w.n - n;
+  }
+  __device__ __forceinline__ int tile(int i) const { return i < a1 ? i : i - a1 + b0; }
+  __device__ __forceinline__ int outer_tile(int e) const { return e < b0 - a1 ? a1 + e : e - (b0 - a1) + b1; }
+};
+
+template <int DT, int D, bool PAGED, bool FOLD>
+__global__ __launch_bounds__(kWinThreads) __attribute__((amdgpu_waves_per_eu(kv4_groups_per_cu(DT, D, FOLD)))) void
+kv4_kernel(const WindowArgs a, const Kv4Cache four) {
   constexpr int PITCH = D + 4;  // accumulator rows start on different banks
-  constexpr int ROWB = D / 2, SROW = D / 32;
-  __shared__ __attribute__((aligned(16))) float lds_acc[kWinWaves][16 * PITCH];
+  constexpr int ROWB = D / 2, SROW = D / 32, COLUMNS = FOLD ? 8 : 16;
+  __shared__ __attribute__((aligned(16))) float lds_acc[kWinWaves][COLUMNS * PITCH];
   __shared__ WinStats ws;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const int lane = threadIdx.x & 63;
   const int n16 = lane & 15;
   const int a4 = lane >> 4;
+  const int col = n16 & (COLUMNS - 1);  // this lane's query row
   const int TG = a.T * a.G;
-  const bool hv = n16 < TG;
-  const int tq = hv ? n16 / a.G : 0;
+  const bool hv = col < TG;
+  const int tq = hv ? col / a.G : 0;
 
   const bool dealt = a.groups > 0;
   int g = blockIdx.y, b = blockIdx.z, part = 0, parts = 1, L;
@@ -274,7 +380,7 @@ __global__ __launch_bounds__(kWinThreads) void kv4_kernel(const WindowArgs a, co
   }
   // the query rows load while the length arrives
   Queries<DT, D> q;
-  q.load(static_cast<const char*>(a.q) + (hv ? out_row(a, b, g, n16) : 0) * (D * (DT == VP_BF16 ? 2 : 4)), hv, a4);
+  q.load(static_cast<const char*>(a.q) + (hv ? out_row(a, b, g, col) : 0) * (D * (DT == VP_BF16 ? 2 : 4)), hv, a4);
   const WindowWalk w(L, a.T, a.window, a.n_sink);
   const int hi = w.L - a.T + tq;                        // this lane's query sees j <= hi
   const int below = a.window > 0 ? hi - a.window : -1;  // and j > below or j < n_sink
@@ -287,193 +393,188 @@ __global__ __launch_bounds__(kWinThreads) void kv4_kernel(const WindowArgs a, co
   const int32_t* bt = PAGED ? a.block_table + static_cast<int64_t>(b) * a.nblk : nullptr;
   const int bmask = PAGED ? (1 << a.bs_log2) - 1 : 0;
 
-  // this part's tiles, and this wave's first one
-  int k = static_cast<int>(static_cast<int64_t>(part) * w.n / parts) + wave;
-  const int k1 = static_cast<int>(static_cast<int64_t>(part + 1) * w.n / parts);
-  // the position read in place of row r of a tile: rows that no query sees are not
-  // read, their places take the nearest row that is read anyway
-  auto row_pos = [&](int t0, int r0, int r1, int r) { return min(max(t0 + r, r0), r1 - 1); };
-  // paged caches: lane r < 32 holds the block of row r
-  auto blocks_of = [&](int k) -> int {
-    int blk = 0;
-    if constexpr (PAGED) {
-      if (k < k1 && lane < 32) blk = bt[row_pos(w.t0(k), w.row_begin(k), w.row_end(k), lane) >> a.bs_log2];
+  const Interior in(w, a.T, a.window);
+
+  auto key = [&](Tile<D>& t, int h, const uint8_t* c, const uint8_t* s) {
+    if constexpr (D == 128) {
+      const uint4 u = *reinterpret_cast<const uint4*>(c + 16 * a4);
+      t.k[h][0] = u.x;
+      t.k[h][1] = u.y;
+      t.k[h][2] = u.z;
+      t.k[h][3] = u.w;
+      t.ks[h] = s[a4];
+    } else {
+      const uint2 u = *reinterpret_cast<const uint2*>(c + 8 * a4);
+      t.k[h][0] = u.x;
+      t.k[h][1] = u.y;
+      t.ks[h] = s[a4 >> 1];
     }
-    return blk;
   };
-  auto load = [&](Tile<D>& t, int k, int blk) {
+  auto value = [&](Tile<D>& t, int i, const uint8_t* c) {
+    if constexpr (D == 128) t.v[i] = reinterpret_cast<const uint32_t*>(c)[n16];
+    else t.v[i] = reinterpret_cast<const uint16_t*>(c)[n16];
+  };
+  // Loads of a tile all of whose rows are read: a half's rows follow each other (blocks
+  // hold at least 16). Paged caches: lanes 0 to 15 hold the first half's block, 16 to 31 the second's.
+  auto load = [&](Tile<D>& t, int t0, int blk) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      int64_t c, s;
+      if constexpr (PAGED) {
+        const int64_t at = __builtin_amdgcn_readlane(blk, 16 * h);
+        const int row = (t0 + 16 * h) & bmask;
+        c = at * four.cb + static_cast<int64_t>(row) * ROWB;
+        s = at * four.sb + static_cast<int64_t>(row) * SROW;
+      } else {
+        c = static_cast<int64_t>(t0 + 16 * h) * ROWB;
+        s = static_cast<int64_t>(t0 + 16 * h) * SROW;
+      }
+      key(t, h, Kc + c + n16 * ROWB, Ks + s + n16 * SROW);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) value(t, 4 * h + i, Vc + c + (4 * a4 + i) * ROWB);
+      if constexpr (D == 128) {
+        const uint4 u = *reinterpret_cast<const uint4*>(Vs + s + 4 * a4 * SROW);
+        t.vs[4 * h] = u.x;
+        t.vs[4 * h + 1] = u.y;
+        t.vs[4 * h + 2] = u.z;
+        t.vs[4 * h + 3] = u.w;
+      } else {
+        const uint2 u = *reinterpret_cast<const uint2*>(Vs + s + 4 * a4 * SROW);
+        t.vs[2 * h] = u.x;
+        t.vs[2 * h + 1] = u.y;
+      }
+    }
+  };
+  auto blocks_of = [&](int t0) -> int {
+    if constexpr (PAGED) return bt[(t0 + (lane & 16)) >> a.bs_log2];
+    else return 0;
+  };
+  // Loads of any tile. Rows that no query sees are not read, their places take the nearest
+  // row that is read anyway.
+  auto load_any = [&](Tile<D>& t, int k) {
     const int t0 = w.t0(k);
     const int r0 = w.row_begin(k), r1 = w.row_end(k);  // rows that some query sees, r0 < r1
-    auto key = [&](int h, const uint8_t* c, const uint8_t* s) {
-      if constexpr (D == 128) {
-        const uint4 u = *reinterpret_cast<const uint4*>(c + 16 * a4);
-        t.k[h][0] = u.x;
-        t.k[h][1] = u.y;
-        t.k[h][2] = u.z;
-        t.k[h][3] = u.w;
-        t.ks[h] = s[a4];
-      } else {
-        const uint2 u = *reinterpret_cast<const uint2*>(c + 8 * a4);
-        t.k[h][0] = u.x;
-        t.k[h][1] = u.y;
-        t.ks[h] = s[a4 >> 1];
+    auto at = [&](int r, int64_t& c, int64_t& s) {
+      const int pos = min(max(t0 + r, r0), r1 - 1);
+      int64_t base = 0;
+      int row = pos;
+      if constexpr (PAGED) {
+        base = bt[pos >> a.bs_log2];
+        row = pos & bmask;
       }
+      c = base * four.cb + static_cast<int64_t>(row) * ROWB;
+      s = base * four.sb + static_cast<int64_t>(row) * SROW;
     };
-    auto value = [&](int i, const uint8_t* c, const uint8_t* s) {
+    int64_t c, s;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      at(16 * h + n16, c, s);
+      key(t, h, Kc + c, Ks + s);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      at(pv_token(a4, i), c, s);
+      value(t, i, Vc + c);
       if constexpr (D == 128) {
-        t.v[i] = reinterpret_cast<const uint32_t*>(c)[n16];
-        t.vs[i] = s[n16 >> 2];
+        t.vs[i] = *reinterpret_cast<const uint32_t*>(Vs + s);
       } else {
-        t.v[i] = reinterpret_cast<const uint16_t*>(c)[n16];
-        t.vs[i] = s[n16 >> 3];
-      }
-    };
-    // row r of the tile: (offset of its codes, of its scales)
-    const bool whole = r0 == t0 && r1 == t0 + 32;
-    if (whole) {
-      // rows of a half follow each other (blocks hold at least 16)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        int64_t c, s;
-        if constexpr (PAGED) {
-          const int64_t at = __builtin_amdgcn_readlane(blk, 16 * h);
-          const int in = (t0 + 16 * h) & bmask;
-          c = at * four.cb + static_cast<int64_t>(in) * ROWB;
-          s = at * four.sb + static_cast<int64_t>(in) * SROW;
-        } else {
-          c = static_cast<int64_t>(t0 + 16 * h) * ROWB;
-          s = static_cast<int64_t>(t0 + 16 * h) * SROW;
-        }
-        key(h, Kc + c + n16 * ROWB, Ks + s + n16 * SROW);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          value(4 * h + i, Vc + c + (4 * a4 + i) * ROWB, Vs + s + (4 * a4 + i) * SROW);
-      }
-    } else {
-      auto at = [&](int r, int64_t& c, int64_t& s) {
-        const int pos = row_pos(t0, r0, r1, r);
-        int64_t base = 0;
-        int in = pos;
-        if constexpr (PAGED) {
-          base = __shfl(blk, r);
-          in = pos & bmask;
-        }
-        c = base * four.cb + static_cast<int64_t>(in) * ROWB;
-        s = base * four.sb + static_cast<int64_t>(in) * SROW;
-      };
-      int64_t c, s;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        at(16 * h + n16, c, s);
-        key(h, Kc + c, Ks + s);
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        at(pv_token(a4, i), c, s);
-        value(i, Vc + c, Vs + s);
+        const uint32_t u = *reinterpret_cast<const uint16_t*>(Vs + s);
+        t.vs[i >> 1] = i & 1 ? t.vs[i >> 1] | u << 16 : u;
       }
     }
   };
 
   float m = kNoLogit, l = 0.f;  // m shared by the four lanes of a query row; l lane-local
-  f32x4 acc[D / 16];
+  Values<D, FOLD> out;
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < out.N; ++i) out.acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  Tile<D> tile, next;
-  int blk = blocks_of(k);
-  if (k < k1) load(tile, k, blk);
-  blk = blocks_of(k + kWinWaves);
-  while (k < k1) {
-    const int t0 = w.t0(k);
-    const bool more = k + kWinWaves < k1;
-    if (more) load(next, k + kWinWaves, blk);
-    blk = blocks_of(k + 2 * kWinWaves);
-
-    // the products q.K, unscaled; value i of this lane is row t0 + pv_token(a4, i)
-    float z[8];
-    {
-      f32x4 c[2];
-      scores<D>(c, tile, q.v);
+  // the products of a tile's rows, unscaled (value i of this lane is row pv_token(a4, i)),
+  // become weights and are added
+  auto attend = [&](const Tile<D>& tile, float (&z)[8]) {
+    float lmax = z[0];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) z[i] = c[i >> 2][i & 3];
-    }
-    // Does every query see every row?
-    const int last0 = w.L - a.T;                                // the first query's own position
-    const int hidden = a.window > 0 ? w.L - 1 - a.window : -1;  // the last query sees no row from n_sink to here
-    const bool edge = t0 + 31 > last0 || max(t0, w.S) <= min(t0 + 31, hidden);
-    unsigned seen = 0xffu;
-    if (edge) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int j = t0 + pv_token(a4, i);
-        if (j > hi || (j <= below && j >= w.S)) seen &= ~(1u << i);
-      }
-    }
-    float lmax = kNegInf;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if ((seen >> i) & 1u) lmax = fmaxf(lmax, z[i]);
+    for (int i = 1; i < 8; ++i) lmax = fmaxf(lmax, z[i]);
     if (__builtin_amdgcn_ballot_w64(lmax > m + a.raise)) {
       // the four lanes of a query row share the reference (their weights meet in one MFMA)
       const float tm = max_over_quads(lmax);
       const bool up = tm > m + a.raise;
       const float al = up ? weight_of(a, m, tm) : 1.f;
       l *= al;
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) acc[i] *= al;
       m = up ? tm : m;
+#pragma unroll
+      for (int i = 0; i < out.N; ++i) out.acc[i] *= al;
     }
     float p[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      p[i] = (seen >> i) & 1u ? weight_of(a, z[i], m) : 0.f;
-      l += p[i];
-    }
-    if (!edge) {
-      values<D>(acc, tile, p);
-    } else {
-      // one query at a time, with the rows that it sees: the others count as zeros
-      // whatever they hold
+    for (int i = 0; i < 8; ++i) p[i] = weight_of(a, z[i], m);
+    l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+    out.add(tile, p, n16);
+  };
+
+  // this part's run of inner tiles, and this wave's first one
+  int i = static_cast<int>(static_cast<int64_t>(part) * in.n / parts) + wave;
+  const int i1 = static_cast<int>(static_cast<int64_t>(part + 1) * in.n / parts);
+  auto first_row = [&](int i) { return w.t0(in.tile(i)); };
+  Tile<D> even, odd;
+  int blk = 0;
+  if (i < i1) load(even, first_row(i), blocks_of(first_row(i)));
+  if (i + kWinWaves < i1) blk = blocks_of(first_row(i + kWinWaves));
+  // The outer tiles, a few at the ends of what is seen, go round the parts
 #pragma unroll 1
-      for (int t = 0; t < a.T; ++t) {
-        const int h = w.L - a.T + t;
-        const int lo = a.window > 0 ? h - a.window : -1;
-        Tile<D> own = tile;
+  for (int e = part + wave * parts; e < in.outer; e += kWinWaves * parts) {
+    const int k = in.outer_tile(e);
+    load_any(odd, k);
+    float z[8];
+    scores<D>(z, odd, q.v);
+    unsigned seen = 0xffu;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int j = t0 + pv_token(a4, i);
-          if (!(j <= h && (j > lo || j < w.S))) {
-            own.v[i] = 0u;
-            own.vs[i] = kScaleMin;
-          }
-        }
-        // (a lane's accumulators are its own query row's: those of other queries are dropped)
-        f32x4 sum[D / 16];
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) sum[i] = acc[i];
-        values<D>(sum, own, p);
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) acc[i] = tq == t ? sum[i] : acc[i];
+    for (int r = 0; r < 8; ++r) {
+      const int j = w.t0(k) + pv_token(a4, r);
+      if (j > hi || (j <= below && j >= w.S)) {
+        seen &= ~(1u << r);
+        z[r] = kNegInf;
       }
     }
-    k += kWinWaves;
-    if (more) tile = next;
+    const unsigned bad = out.take_nan(odd, n16);
+    attend(odd, z);
+    if (__builtin_amdgcn_ballot_w64(bad != 0)) out.put_nan(bad, seen);
+  }
+  // tile i is in `tile`, the wave's next one is requested into `next`
+  auto step = [&](const Tile<D>& tile, Tile<D>& next) {
+    i += kWinWaves;
+    if (i < i1) load(next, first_row(i), blk);
+    if (i + kWinWaves < i1) blk = blocks_of(first_row(i + kWinWaves));
+    float z[8];
+    scores<D>(z, tile, q.v);
+    attend(tile, z);
+  };
+#pragma unroll 1
+  while (i < i1) {
+    step(even, odd);
+    if (i >= i1) break;
+    step(odd, even);
   }
   l = sum_over_quads(l);
 
   // ---- join the four waves ----
-  if (a4 == 0) {
+  if (a4 == 0 && n16 < COLUMNS) {
     ws.m[wave][n16] = m;
     ws.l[wave][n16] = l;
   }
-  // acc[e][r] holds dim (D/16) (4 a4 + r) + e
-  float* mine = lds_acc[wave] + n16 * PITCH;
+  float* mine = lds_acc[wave] + col * PITCH;
 #pragma unroll
-  for (int r = 0; r < 4; ++r)
+  for (int r = 0; r < 4; ++r) {
+    if constexpr (FOLD) {
 #pragma unroll
-    for (int e = 0; e < D / 16; e += 4)
-      *reinterpret_cast<float4*>(mine + (D / 16) * (4 * a4 + r) + e) = make_float4(acc[e][r], acc[e + 1][r], acc[e + 2][r], acc[e + 3][r]);
+      for (int i = 0; i < out.N; ++i) mine[(D / 16) * (4 * a4 + r) + 2 * i + (n16 >> 3)] = out.acc[i][r];
+    } else {
+#pragma unroll
+      for (int e = 0; e < out.N; e += 4)
+        *reinterpret_cast<float4*>(mine + (D / 16) * (4 * a4 + r) + e) =
+            make_float4(out.acc[e][r], out.acc[e + 1][r], out.acc[e + 2][r], out.acc[e + 3][r]);
+    }
+  }
   __syncthreads();
   const size_t pair = static_cast<size_t>(b) * a.Hkv + g;
   const size_t piece0 = static_cast<size_t>(blockIdx.x) * TG;
@@ -511,8 +612,11 @@ __global__ __launch_bounds__(kWinThreads) void kv4_kernel(const WindowArgs a, co
 template <int DT, int D>
 hipError_t attention_dd(const WindowArgs& a, const Kv4Cache& four, hipStream_t st) {
   const dim3 grid = a.groups > 0 ? dim3(a.groups) : dim3(1, a.Hkv, a.B);
-  if (a.bs_log2 >= 0) hipLaunchKernelGGL((kv4_kernel<DT, D, true>), grid, dim3(kWinThreads), 0, st, a, four);
-  else hipLaunchKernelGGL((kv4_kernel<DT, D, false>), grid, dim3(kWinThreads), 0, st, a, four);
+  const bool paged = a.bs_log2 >= 0, fold = a.T * a.G <= 8;
+  if (paged && fold) hipLaunchKernelGGL((kv4_kernel<DT, D, true, true>), grid, dim3(kWinThreads), 0, st, a, four);
+  else if (paged) hipLaunchKernelGGL((kv4_kernel<DT, D, true, false>), grid, dim3(kWinThreads), 0, st, a, four);
+  else if (fold) hipLaunchKernelGGL((kv4_kernel<DT, D, false, true>), grid, dim3(kWinThreads), 0, st, a, four);
+  else hipLaunchKernelGGL((kv4_kernel<DT, D, false, false>), grid, dim3(kWinThreads), 0, st, a, four);
   return hipGetLastError();
 }
 
@@ -531,7 +635,7 @@ WindowPlan make_kv4_plan(const vp_shape& s, const vp_window& w) {
   const bool cut = w.window > 0 && 2 * tiles <= cap;
   const bool brief = 2400 * tiles <= pairs * (350 + s.batch);
   const bool one_each = tiles <= 16 || brief || (cut && pairs >= 512) || pairs * tiles > 0x3fffffff;
-  const int64_t most = std::max<int64_t>(1024, 2 * pairs);
+  const int64_t most = std::max<int64_t>(512, 2 * pairs);
   p.groups = one_each ? 0 : static_cast<int>(std::min(most, pairs * ((tiles + kWinWaves - 1) / kWinWaves)));
   carve_window_plan(p, s, false);
   return p;
