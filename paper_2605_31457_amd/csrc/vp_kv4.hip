@@ -12,10 +12,9 @@
 // exact products; fp32 queries enter as three bf16 numbers, all 24 bits of them. Values: the
 // weights as three bf16 numbers (as in value_product).
 //
-// The walk, its masks, its running maximum and its parts are those of window_kernel. The
-// rows go to registers, not through LDS: a lane's 16 bytes of a key are one block of 32
-// elements with one scale, which is what its slots of the products take, and the 4 bytes that
-// it takes of a value row are 8 elements, for the 8 products that it takes part in.
+// The walk, its masks, its running maximum and its parts are those of window_kernel. A
+// wave has places for three tiles of 32 rows in LDS: while one is worked on, the next two
+// tiles' copies are on their way.
 #include <algorithm>
 #include <type_traits>
 
@@ -162,36 +161,69 @@ struct Queries {
   }
 };
 
-// what a lane holds of a tile of 32 rows
+// A tile of 32 rows in LDS: K codes, V codes, rows one after another as in memory, but for
+// the 16-byte pieces of a row of 64 bytes, which change places (at): so that the 16 rows that
+// a product's operand takes do not meet on the same banks.
 template <int D>
-struct Tile {
-  static constexpr int KW = D / 32;  // dwords of a key row's piece, its dims (D/4) a4 ..
-  static constexpr int VS = D / 16;  // dwords of the value rows' scales
-  uint32_t k[2][KW];                 // rows 16 half + n16
-  uint32_t ks[2];                    // their scale bytes
-  uint32_t v[8];                     // rows pv_token(a4, i): elements (D/16) n16 ..
-  uint32_t vs[VS];                   // all their scales: row i in dword i (D = 128), in half i % 2 of dword i / 2
+struct Tile4 {
+  static constexpr int ROWB = D / 2, SROW = D / 32;
+  static constexpr int BYTES = 32 * ROWB;          // of K or V
+  static constexpr int COPIES = BYTES / 1024;      // copy instructions of K or V
+  static constexpr int REQUESTS = 2 * COPIES + 1;  // of a tile, that of its scales among them
+  static __device__ __forceinline__ int at(int row, int piece) {
+    return row * ROWB + 16 * (D == 128 ? piece ^ (row >> 2 & 3) : piece);
+  }
 };
 
-// A value row's scale: a lane's elements lie in one block of 32, whose byte comes to bits 23 to 30
+// The row in a lane's slot i of the products: a key operand's row n16 of half h is the tile's
+// row 16 h + 4 (n16 % 4) + n16 / 4, so that its score ends up where the lane's four values of
+// an instruction are 4 neighbouring rows over the four lanes.
+__device__ __forceinline__ int slot_row(int a4, int i) { return 16 * (i >> 2) + 4 * (i & 3) + a4; }
+
+// The scales' places in LDS, a dword per row: those of a lane's slots side by side
+__device__ __forceinline__ int scale_place(int row) { return (row & 16) + 4 * (row & 3) + ((row >> 2) & 3); }
+
+// byte `b` of a row's scales, at bits 23 to 30
+__device__ __forceinline__ float scale_at(uint32_t scales, int b) {
+  return __uint_as_float(__builtin_amdgcn_alignbit(scales, scales, (8 * b + 9) & 31));
+}
+
+// A lane's pieces of two key rows 16 rows apart. Written by hand, because for one of the three
+// places the compiler waits for all copies in flight before it (64 contexts of 32k tokens:
+// 194 us, so 190).
 template <int D>
-__device__ __forceinline__ uint32_t value_scale(const Tile<D>& t, int i, int n16) {
-  if constexpr (D == 128) return __builtin_amdgcn_alignbit(t.vs[i], t.vs[i], (8 * (n16 >> 2) + 9) & 31);
-  else return __builtin_amdgcn_alignbit(t.vs[i >> 1], t.vs[i >> 1], (8 * (n16 >> 3) + 16 * (i & 1) + 9) & 31);
+__device__ __forceinline__ void key_pieces(uint32_t (&u)[2][D / 32], const unsigned char* p) {
+#ifdef __HIP_DEVICE_COMPILE__
+  typedef unsigned uints __attribute__((ext_vector_type(D / 32)));
+  uints x, y;
+  const uint32_t at = (uint32_t)(uintptr_t)(lds_byte*)p;
+  if constexpr (D == 128)
+    asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %2 offset:1024\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x), "=&v"(y) : "v"(at) : "memory");
+  else
+    asm volatile("ds_read_b64 %0, %2\n\tds_read_b64 %1, %2 offset:512\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x), "=&v"(y) : "v"(at) : "memory");
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+    u[0][i] = x[i];
+    u[1][i] = y[i];
+  }
+#endif
 }
 
 template <int D, int N>
-__device__ __forceinline__ void scores(float (&z)[8], const Tile<D>& t, const bf16x8 (&q)[N][D / 32]) {
+__device__ __forceinline__ void scores(float (&z)[8], const unsigned char* kb, const uint32_t* ks, const bf16x8 (&q)[N][D / 32],
+                                       int a4, int n16) {
+  const uint32_t byte[2] = {ks[n16], ks[16 + n16]};
+  uint32_t u[2][D / 32];
+  const int row = 4 * (n16 & 3) + (n16 >> 2);
+  key_pieces<D>(u, kb + (D == 128 ? Tile4<D>::at(row, a4) : row * 32 + 8 * a4));
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const float scale = scale_of(t.ks[h]);
+    const float scale = scale_at(byte[h], D == 128 ? a4 : a4 >> 1);
     f32x4 c = {0.f, 0.f, 0.f, 0.f};
     bf16x8 k[D / 32];
 #pragma unroll
-    for (int s = 0; s < D / 32; ++s) {
-      const uint32_t u = t.k[h][s];
-      k[s] = __builtin_bit_cast(bf16x8, make_uint4(two_of<0>(u, scale), two_of<1>(u, scale), two_of<2>(u, scale), two_of<3>(u, scale)));
-    }
+    for (int s = 0; s < D / 32; ++s)
+      k[s] = __builtin_bit_cast(bf16x8, make_uint4(two_of<0>(u[h][s], scale), two_of<1>(u[h][s], scale), two_of<2>(u[h][s], scale), two_of<3>(u[h][s], scale)));
 #pragma unroll
     for (int p = N - 1; p >= 0; --p)
 #pragma unroll
@@ -200,6 +232,44 @@ __device__ __forceinline__ void scores(float (&z)[8], const Tile<D>& t, const bf
     for (int r = 0; r < 4; ++r) z[4 * h + r] = c[r];
   }
 }
+
+// what a lane holds of a tile's values: the rows of its slots, elements (D/16) n16 ..
+template <int D>
+struct ValueRows {
+  uint32_t v[8];
+  float scale[8];
+  __device__ __forceinline__ void load(const unsigned char* vb, const uint32_t* vs, int a4, int n16) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int row = slot_row(a4, i);
+      if constexpr (D == 128) v[i] = *reinterpret_cast<const uint32_t*>(vb + row * 64 + 16 * ((n16 >> 2) ^ (i & 3)) + 4 * (n16 & 3));
+      else v[i] = *reinterpret_cast<const uint16_t*>(vb + row * 32 + 2 * n16);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint4 x = *reinterpret_cast<const uint4*>(vs + 16 * h + 4 * a4);
+      const int b = D == 128 ? n16 >> 2 : n16 >> 3;  // (a lane's elements lie in one block of 32)
+      scale[4 * h] = scale_at(x.x, b);
+      scale[4 * h + 1] = scale_at(x.y, b);
+      scale[4 * h + 2] = scale_at(x.z, b);
+      scale[4 * h + 3] = scale_at(x.w, b);
+    }
+  }
+  // Tiles where some query does not see some row: blocks of NaN would reach the outputs of
+  // the queries that do not see them as 0 NaN. They are taken out (bit i of the result: this
+  // lane's block of row i is one), ...
+  __device__ __forceinline__ unsigned take_nan() {
+    unsigned bad = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bool b = (__float_as_uint(scale[i]) & 0x7f800000u) == 0x7f800000u;
+      bad |= b ? 1u << i : 0u;
+      v[i] = b ? 0u : v[i];
+      scale[i] = b ? 1.f : scale[i];
+    }
+    return bad;
+  }
+};
 
 // The value product. The weights enter as the sum of three bf16 numbers, all 24 bits of
 // them (truncated one after another: exact).
@@ -220,13 +290,13 @@ struct Values {
     return p - __uint_as_float(__float_as_uint(p) & 0xffff0000u);
   }
   template <int B>
-  __device__ __forceinline__ void byte(const Tile<D>& t, const float (&scale)[8], const bf16x8 (&w)[FOLD ? 6 : 3]) {
+  __device__ __forceinline__ void byte(const ValueRows<D>& t, const bf16x8 (&w)[FOLD ? 6 : 3]) {
     if constexpr (FOLD) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         uint32_t x[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = two_of<B>(t.v[4 * h + j], scale[4 * h + j]);
+        for (int j = 0; j < 4; ++j) x[j] = two_of<B>(t.v[4 * h + j], t.scale[4 * h + j]);
         const bf16x8 a = __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
 #pragma unroll
         for (int i = 0; i < 3; ++i) acc[B] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[3 * h + i], acc[B], 0, 0, 0);
@@ -235,7 +305,7 @@ struct Values {
       uint32_t lo[4], hi[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint32_t x = two_of<B>(t.v[2 * j], scale[2 * j]), y = two_of<B>(t.v[2 * j + 1], scale[2 * j + 1]);
+        const uint32_t x = two_of<B>(t.v[2 * j], t.scale[2 * j]), y = two_of<B>(t.v[2 * j + 1], t.scale[2 * j + 1]);
         lo[j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
         hi[j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
       }
@@ -248,8 +318,8 @@ struct Values {
       }
     }
   }
-  // p: the weights of rows pv_token(a4, i)
-  __device__ __forceinline__ void add(const Tile<D>& t, const float (&p)[8], int n16) {
+  // p: the weights of the lane's rows
+  __device__ __forceinline__ void add(const ValueRows<D>& t, const float (&p)[8], int n16) {
     bf16x8 w[FOLD ? 6 : 3];
     float x[8];
 #pragma unroll
@@ -272,37 +342,14 @@ struct Values {
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = rest(x[i]);
     }
-    float scale[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) scale[i] = __uint_as_float(value_scale<D>(t, i, n16));
-    byte<0>(t, scale, w);
-    byte<1>(t, scale, w);
+    byte<0>(t, w);
+    byte<1>(t, w);
     if constexpr (D == 128) {
-      byte<2>(t, scale, w);
-      byte<3>(t, scale, w);
+      byte<2>(t, w);
+      byte<3>(t, w);
     }
   }
-  // Tiles where some query does not see some row: blocks of NaN would reach the outputs of
-  // the queries that do not see them as 0 NaN. They are taken out of the tile (bit i of the
-  // result: this lane's block of row i is one), ...
-  __device__ __forceinline__ static unsigned take_nan(Tile<D>& t, int n16) {
-    unsigned bad = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const bool b = (value_scale<D>(t, i, n16) & 0x7f800000u) == 0x7f800000u;
-      bad |= b ? 1u << i : 0u;
-      t.v[i] = b ? 0u : t.v[i];
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      // (the lane's byte of that row's scales becomes 2^0; others are not this lane's to read)
-      const int at = D == 128 ? 8 * (n16 >> 2) : 8 * (n16 >> 3) + 16 * (i & 1);
-      uint32_t& s = t.vs[D == 128 ? i : i >> 1];
-      if ((bad >> i) & 1u) s = (s & ~(0xffu << at)) | 127u << at;
-    }
-    return bad;
-  }
-  // ... and the queries that do see one get NaN: by the number of such rows, a product of
+  // ... (ValueRows::take_nan) and the queries that do see one get NaN: by the number of such rows, a product of
   // zeros and ones
   __device__ __forceinline__ void put_nan(unsigned bad, unsigned seen) {
     f32x4 count = {0.f, 0.f, 0.f, 0.f};
@@ -352,9 +399,19 @@ struct Interior {
 template <int DT, int D, bool PAGED, bool FOLD>
 __global__ __launch_bounds__(kWinThreads) __attribute__((amdgpu_waves_per_eu(kv4_groups_per_cu(DT, D, FOLD)))) void
 kv4_kernel(const WindowArgs a, const Kv4Cache four) {
-  constexpr int PITCH = D + 4;  // accumulator rows start on different banks
-  constexpr int ROWB = D / 2, SROW = D / 32, COLUMNS = FOLD ? 8 : 16;
-  __shared__ __attribute__((aligned(16))) float lds_acc[kWinWaves][COLUMNS * PITCH];
+  using Q = Tile4<D>;
+  constexpr int COLUMNS = FOLD ? 8 : 16;
+  // Per wave: places for the K codes, and for the V codes and scales, of three tiles (after the
+  // walk the first tile's make room for half of the accumulator rows each). Arrays of their
+  // own: in one, the compiler would have reads of a tile wait for the copies of another (it
+  // tells up to 8 arrays apart).
+  constexpr int FIRST = max_i(Q::BYTES, COLUMNS / 2 * D * 4), SCALES = 64 * 4;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds_k0[kWinWaves * FIRST];
+  __shared__ __attribute__((aligned(1024))) unsigned char lds_v0[kWinWaves * (FIRST + SCALES)];
+  __shared__ __attribute__((aligned(1024))) unsigned char lds_k1[kWinWaves * Q::BYTES];
+  __shared__ __attribute__((aligned(1024))) unsigned char lds_v1[kWinWaves * (Q::BYTES + SCALES)];
+  __shared__ __attribute__((aligned(1024))) unsigned char lds_k2[kWinWaves * Q::BYTES];
+  __shared__ __attribute__((aligned(1024))) unsigned char lds_v2[kWinWaves * (Q::BYTES + SCALES)];
   __shared__ WinStats ws;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const int lane = threadIdx.x & 63;
@@ -388,100 +445,88 @@ kv4_kernel(const WindowArgs a, const Kv4Cache four) {
   const int64_t seq_c = (PAGED ? 0 : b * four.cb) + g * four.ch, seq_s = (PAGED ? 0 : b * four.sb) + g * four.sh;
   const uint8_t* const Kc = four.kc + seq_c;
   const uint8_t* const Vc = four.vc + seq_c;
-  const uint8_t* const Ks = four.ks + seq_s;
-  const uint8_t* const Vs = four.vs + seq_s;
   const int32_t* bt = PAGED ? a.block_table + static_cast<int64_t>(b) * a.nblk : nullptr;
   const int bmask = PAGED ? (1 << a.bs_log2) - 1 : 0;
-
   const Interior in(w, a.T, a.window);
+  unsigned char* const k0 = lds_k0 + wave * FIRST;
+  unsigned char* const v0 = lds_v0 + wave * (FIRST + SCALES);
+  unsigned char* const k1 = lds_k1 + wave * Q::BYTES;
+  unsigned char* const v1 = lds_v1 + wave * (Q::BYTES + SCALES);
+  unsigned char* const k2 = lds_k2 + wave * Q::BYTES;
+  unsigned char* const v2 = lds_v2 + wave * (Q::BYTES + SCALES);
 
-  auto key = [&](Tile<D>& t, int h, const uint8_t* c, const uint8_t* s) {
-    if constexpr (D == 128) {
-      const uint4 u = *reinterpret_cast<const uint4*>(c + 16 * a4);
-      t.k[h][0] = u.x;
-      t.k[h][1] = u.y;
-      t.k[h][2] = u.z;
-      t.k[h][3] = u.w;
-      t.ks[h] = s[a4];
+  // Copies: lane i of an instruction fills bytes 16 i .. of 1 KB, so it takes one piece of
+  // one row. Scales: a dword per row (of 64: their two bytes), key rows by lanes 0 to 31, value
+  // rows by the others.
+  const int copy_row = lane / (Q::ROWB / 16);
+  const int copy_piece = (Q::at(copy_row, lane % (Q::ROWB / 16)) - copy_row * Q::ROWB) / 16;
+  const uint32_t copy_off = copy_row * Q::ROWB + 16 * copy_piece;
+  const int scale_row = scale_place(lane & 31);  // (its own inverse)
+  const uint8_t* const scale_src = (lane < 32 ? four.ks : four.vs) + seq_s;
+  auto copy = [&](const uint8_t* src, unsigned char* dst) {
+    __builtin_amdgcn_global_load_lds((global_void*)src, (lds_void*)(lds_byte*)dst, 16, 0, kCopyPolicy);
+  };
+  auto scales_at = [&](unsigned char* vb) { return reinterpret_cast<const uint32_t*>(vb + Q::BYTES); };
+  auto copy_scales = [&](const uint8_t* src, unsigned char* dst) {
+    __builtin_amdgcn_global_load_lds((global_void*)src, (lds_void*)(lds_byte*)dst, Q::SROW, 0, kCopyPolicy);
+  };
+  // Paged caches: the blocks of a tile's halves (a half's rows follow each other: blocks
+  // hold at least 16). Scalar loads, so that no wait for one is a wait for copies.
+  typedef __attribute__((address_space(4))) const int32_t table_entry;
+  auto blocks_of = [&](int t0) -> int2 {
+    if constexpr (PAGED) {
+      const table_entry* t = (const table_entry*)bt;
+      return make_int2(t[t0 >> a.bs_log2], t[(t0 + 16) >> a.bs_log2]);
     } else {
-      const uint2 u = *reinterpret_cast<const uint2*>(c + 8 * a4);
-      t.k[h][0] = u.x;
-      t.k[h][1] = u.y;
-      t.ks[h] = s[a4 >> 1];
+      return make_int2(0, 0);
     }
   };
-  auto value = [&](Tile<D>& t, int i, const uint8_t* c) {
-    if constexpr (D == 128) t.v[i] = reinterpret_cast<const uint32_t*>(c)[n16];
-    else t.v[i] = reinterpret_cast<const uint16_t*>(c)[n16];
-  };
-  // Loads of a tile all of whose rows are read: a half's rows follow each other (blocks
-  // hold at least 16). Paged caches: lanes 0 to 15 hold the first half's block, 16 to 31 the second's.
-  auto load = [&](Tile<D>& t, int t0, int blk) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      int64_t c, s;
-      if constexpr (PAGED) {
-        const int64_t at = __builtin_amdgcn_readlane(blk, 16 * h);
-        const int row = (t0 + 16 * h) & bmask;
-        c = at * four.cb + static_cast<int64_t>(row) * ROWB;
-        s = at * four.sb + static_cast<int64_t>(row) * SROW;
-      } else {
-        c = static_cast<int64_t>(t0 + 16 * h) * ROWB;
-        s = static_cast<int64_t>(t0 + 16 * h) * SROW;
-      }
-      key(t, h, Kc + c + n16 * ROWB, Ks + s + n16 * SROW);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) value(t, 4 * h + i, Vc + c + (4 * a4 + i) * ROWB);
+  // Requests the tile at row t0, all of whose rows are read
+  auto request = [&](int t0, int2 blk, unsigned char* kb, unsigned char* vb) {
+    if constexpr (PAGED) {
+      const int r0 = t0 & bmask, r1 = (t0 + 16) & bmask;
+      const int64_t c0 = blk.x * four.cb + static_cast<int64_t>(r0) * Q::ROWB, c1 = blk.y * four.cb + static_cast<int64_t>(r1) * Q::ROWB;
       if constexpr (D == 128) {
-        const uint4 u = *reinterpret_cast<const uint4*>(Vs + s + 4 * a4 * SROW);
-        t.vs[4 * h] = u.x;
-        t.vs[4 * h + 1] = u.y;
-        t.vs[4 * h + 2] = u.z;
-        t.vs[4 * h + 3] = u.w;
+        copy(Kc + c0 + copy_off, kb);
+        copy(Kc + c1 + copy_off, kb + 1024);
+        copy(Vc + c0 + copy_off, vb);
+        copy(Vc + c1 + copy_off, vb + 1024);
       } else {
-        const uint2 u = *reinterpret_cast<const uint2*>(Vs + s + 4 * a4 * SROW);
-        t.vs[2 * h] = u.x;
-        t.vs[2 * h + 1] = u.y;
+        const int64_t c = (lane < 32 ? c0 : c1 - 16 * Q::ROWB) + copy_off;
+        copy(Kc + c, kb);
+        copy(Vc + c, vb);
       }
+      const int64_t at0 = blk.x * four.sb + static_cast<int64_t>(r0) * Q::SROW, at1 = blk.y * four.sb + static_cast<int64_t>(r1 - 16) * Q::SROW;
+      copy_scales(scale_src + ((lane & 16) == 0 ? at0 : at1) + scale_row * Q::SROW, vb + Q::BYTES);
+    } else {
+      const int64_t c = static_cast<int64_t>(t0) * Q::ROWB;
+#pragma unroll
+      for (int j = 0; j < Q::COPIES; ++j) copy(Kc + c + (copy_off + 1024 * j), kb + 1024 * j);
+#pragma unroll
+      for (int j = 0; j < Q::COPIES; ++j) copy(Vc + c + (copy_off + 1024 * j), vb + 1024 * j);
+      copy_scales(scale_src + static_cast<int64_t>(t0) * Q::SROW + scale_row * Q::SROW, vb + Q::BYTES);
     }
   };
-  auto blocks_of = [&](int t0) -> int {
-    if constexpr (PAGED) return bt[(t0 + (lane & 16)) >> a.bs_log2];
-    else return 0;
-  };
-  // Loads of any tile. Rows that no query sees are not read, their places take the nearest
+  // Requests any tile. Rows that no query sees are not read, their places take the nearest
   // row that is read anyway.
-  auto load_any = [&](Tile<D>& t, int k) {
+  auto request_any = [&](int k, unsigned char* kb, unsigned char* vb) {
     const int t0 = w.t0(k);
     const int r0 = w.row_begin(k), r1 = w.row_end(k);  // rows that some query sees, r0 < r1
-    auto at = [&](int r, int64_t& c, int64_t& s) {
+    auto place = [&](int r, int64_t& block) {
       const int pos = min(max(t0 + r, r0), r1 - 1);
-      int64_t base = 0;
-      int row = pos;
-      if constexpr (PAGED) {
-        base = bt[pos >> a.bs_log2];
-        row = pos & bmask;
-      }
-      c = base * four.cb + static_cast<int64_t>(row) * ROWB;
-      s = base * four.sb + static_cast<int64_t>(row) * SROW;
+      block = PAGED ? bt[pos >> a.bs_log2] : 0;
+      return PAGED ? pos & bmask : pos;
     };
-    int64_t c, s;
+    int64_t block;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      at(16 * h + n16, c, s);
-      key(t, h, Kc + c, Ks + s);
+    for (int j = 0; j < Q::COPIES; ++j) {
+      const int row = place(1024 / Q::ROWB * j + copy_row, block);
+      const int64_t c = block * four.cb + static_cast<int64_t>(row) * Q::ROWB + 16 * copy_piece;
+      copy(Kc + c, kb + 1024 * j);
+      copy(Vc + c, vb + 1024 * j);
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      at(pv_token(a4, i), c, s);
-      value(t, i, Vc + c);
-      if constexpr (D == 128) {
-        t.vs[i] = *reinterpret_cast<const uint32_t*>(Vs + s);
-      } else {
-        const uint32_t u = *reinterpret_cast<const uint16_t*>(Vs + s);
-        t.vs[i >> 1] = i & 1 ? t.vs[i >> 1] | u << 16 : u;
-      }
-    }
+    const int row = place(scale_row, block);
+    copy_scales(scale_src + block * four.sb + static_cast<int64_t>(row) * Q::SROW, vb + Q::BYTES);
   };
 
   float m = kNoLogit, l = 0.f;  // m shared by the four lanes of a query row; l lane-local
@@ -489,9 +534,9 @@ kv4_kernel(const WindowArgs a, const Kv4Cache four) {
 #pragma unroll
   for (int i = 0; i < out.N; ++i) out.acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  // the products of a tile's rows, unscaled (value i of this lane is row pv_token(a4, i)),
-  // become weights and are added
-  auto attend = [&](const Tile<D>& tile, float (&z)[8]) {
+  // the products of a tile's rows, unscaled (value i of this lane is row slot_row(a4, i)),
+  // become weights, and the values are added
+  auto weigh = [&](float (&z)[8]) {
     float lmax = z[0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) lmax = fmaxf(lmax, z[i]);
@@ -505,55 +550,77 @@ kv4_kernel(const WindowArgs a, const Kv4Cache four) {
 #pragma unroll
       for (int i = 0; i < out.N; ++i) out.acc[i] *= al;
     }
-    float p[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) p[i] = weight_of(a, z[i], m);
-    l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-    out.add(tile, p, n16);
+    for (int i = 0; i < 8; ++i) z[i] = weight_of(a, z[i], m);
+    l += ((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]));
   };
 
   // this part's run of inner tiles, and this wave's first one
   int i = static_cast<int>(static_cast<int64_t>(part) * in.n / parts) + wave;
   const int i1 = static_cast<int>(static_cast<int64_t>(part + 1) * in.n / parts);
   auto first_row = [&](int i) { return w.t0(in.tile(i)); };
-  Tile<D> even, odd;
-  int blk = 0;
-  if (i < i1) load(even, first_row(i), blocks_of(first_row(i)));
-  if (i + kWinWaves < i1) blk = blocks_of(first_row(i + kWinWaves));
+  auto own_row = [&](int n) { return first_row(min(i + n * kWinWaves, i1 - 1)); };  // the wave's n-th tile from here, or the last
+  int2 blk{};  // of the next tile to be requested
+  if (i < i1) {
+    request(own_row(0), blocks_of(own_row(0)), k0, v0);
+    if (i + kWinWaves < i1) request(own_row(1), blocks_of(own_row(1)), k1, v1);
+    blk = blocks_of(own_row(2));
+  }
   // The outer tiles, a few at the ends of what is seen, go round the parts
 #pragma unroll 1
   for (int e = part + wave * parts; e < in.outer; e += kWinWaves * parts) {
     const int k = in.outer_tile(e);
-    load_any(odd, k);
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+    request_any(k, k2, v2);
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
     float z[8];
-    scores<D>(z, odd, q.v);
+    scores<D>(z, k2, scales_at(v2), q.v, a4, n16);
     unsigned seen = 0xffu;
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
-      const int j = w.t0(k) + pv_token(a4, r);
+      const int j = w.t0(k) + slot_row(a4, r);
       if (j > hi || (j <= below && j >= w.S)) {
         seen &= ~(1u << r);
         z[r] = kNegInf;
       }
     }
-    const unsigned bad = out.take_nan(odd, n16);
-    attend(odd, z);
+    weigh(z);
+    ValueRows<D> rows;
+    rows.load(v2, scales_at(v2) + 32, a4, n16);
+    const unsigned bad = rows.take_nan();
+    out.add(rows, z, n16);
     if (__builtin_amdgcn_ballot_w64(bad != 0)) out.put_nan(bad, seen);
   }
-  // tile i is in `tile`, the wave's next one is requested into `next`
-  auto step = [&](const Tile<D>& tile, Tile<D>& next) {
-    i += kWinWaves;
-    if (i < i1) load(next, first_row(i), blk);
-    if (i + kWinWaves < i1) blk = blocks_of(first_row(i + kWinWaves));
+  // Tile i is at (kb, vb), or on its way there, and so is the wave's next one at places of
+  // its own; the one after is requested into the third. Memory operations of a wave complete
+  // in the order of their issue: a wait names how many issued after what it waits for may be
+  // left.
+  auto step = [&](unsigned char* kb, unsigned char* vb, unsigned char* k_next, unsigned char* v_next) {
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm0);  // reads of the third place have returned
+    if (i + 2 * kWinWaves < i1) {
+      request(own_row(2), blk, k_next, v_next);
+      blk = blocks_of(own_row(3));
+      __builtin_amdgcn_s_waitcnt(wait_vm(2 * Q::REQUESTS));
+    } else if (i + kWinWaves < i1) {
+      __builtin_amdgcn_s_waitcnt(wait_vm(Q::REQUESTS));
+    } else {
+      __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    }
     float z[8];
-    scores<D>(z, tile, q.v);
-    attend(tile, z);
+    scores<D>(z, kb, scales_at(vb), q.v, a4, n16);
+    weigh(z);
+    ValueRows<D> rows;
+    rows.load(vb, scales_at(vb) + 32, a4, n16);
+    out.add(rows, z, n16);
+    i += kWinWaves;
   };
 #pragma unroll 1
   while (i < i1) {
-    step(even, odd);
+    step(k0, v0, k2, v2);
     if (i >= i1) break;
-    step(odd, even);
+    step(k1, v1, k0, v0);
+    if (i >= i1) break;
+    step(k2, v2, k1, v1);
   }
   l = sum_over_quads(l);
 
@@ -562,7 +629,8 @@ kv4_kernel(const WindowArgs a, const Kv4Cache four) {
     ws.m[wave][n16] = m;
     ws.l[wave][n16] = l;
   }
-  float* mine = lds_acc[wave] + col * PITCH;
+  __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+  float* mine = reinterpret_cast<float*>(col < COLUMNS / 2 ? k0 : v0) + col % (COLUMNS / 2) * D;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     if constexpr (FOLD) {
@@ -589,7 +657,7 @@ kv4_kernel(const WindowArgs a, const Kv4Cache four) {
 #pragma unroll
     for (int v = 0; v < kWinWaves; ++v) {
       const float f = weight_of(a, ws.m[v][h], M);
-      const float4 x = reinterpret_cast<const float4*>(lds_acc[v] + h * PITCH)[c];
+      const float4 x = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(h < COLUMNS / 2 ? lds_k0 + v * FIRST : lds_v0 + v * (FIRST + SCALES)) + h % (COLUMNS / 2) * D)[c];
       den = fmaf(f, ws.l[v][h], den);
       o.x = fmaf(f, x.x, o.x);
       o.y = fmaf(f, x.y, o.y);

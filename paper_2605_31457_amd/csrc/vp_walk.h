@@ -5,11 +5,25 @@
 #include "vp_blocks.h"
 #include "vp_cache.h"
 #include "vp_common.h"
+#include "vp_tile.h"
 
 namespace vp {
 
 constexpr int kWinWaves = 4;
 constexpr int kWinThreads = 64 * kWinWaves;
+
+// s_waitcnt operand: at most n vector memory operations left (n < 64), others unconstrained
+constexpr int wait_vm(int n) { return kWaitVm0 | (n & 15) | (n >> 4) << 14; }
+
+// A float to the stage. Written by hand, because the compiler may have any LDS store wait
+// for all copies in flight (fp32 rows of 128, 8 x 16k with sums: 111 us, so 108). A wave's LDS
+// accesses happen in order, so its reads of the stage need nothing else.
+__device__ __forceinline__ void stage_store(float* p, float x) {
+#ifdef __HIP_DEVICE_COMPILE__
+  typedef __attribute__((address_space(3))) float lds_float;
+  asm volatile("ds_write_b32 %0, %1" ::"v"((uint32_t)(uintptr_t)(lds_float*)p), "v"(x) : "memory");
+#endif
+}
 
 inline size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 

@@ -53,9 +53,6 @@
 namespace vp {
 namespace {
 
-// s_waitcnt operand: at most n vector memory operations left (n < 64), others unconstrained
-constexpr int wait_vm(int n) { return kWaitVm0 | (n & 15) | (n >> 4) << 14; }
-
 template <int DT, int D, bool SUMS>
 struct WinLds {
   using C = Cfg<DT, D>;
@@ -106,16 +103,6 @@ struct EvenCopy {
                                                kCopyPolicy);
   }
 };
-
-// A float to the stage. Written by hand, because the compiler may have any LDS store wait
-// for all copies in flight (fp32 rows of 128, 8 x 16k with sums: 111 us, so 108). A wave's LDS
-// accesses happen in order, so its reads of the stage need nothing else.
-__device__ __forceinline__ void stage_store(float* p, float x) {
-#ifdef __HIP_DEVICE_COMPILE__
-  typedef __attribute__((address_space(3))) float lds_float;
-  asm volatile("ds_write_b32 %0, %1" ::"v"((uint32_t)(uintptr_t)(lds_float*)p), "v"(x) : "memory");
-#endif
-}
 
 // a tile's logits, 32 rows of gp floats, from the stage to the plane
 struct StoreLogits {
