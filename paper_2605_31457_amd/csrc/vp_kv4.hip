@@ -161,9 +161,9 @@ struct Queries {
   }
 };
 
-// A tile of 32 rows in LDS: K codes, V codes, rows one after another as in memory, but for
-// the 16-byte pieces of a row of 64 bytes, which change places (at): so that the 16 rows that
-// a product's operand takes do not meet on the same banks.
+// A tile of 32 rows in LDS: K codes and V codes, rows one after another as in memory, but for
+// the 16-byte pieces of a key row of 64 bytes, which change places (at), so that the 16 rows that
+// a product's operand takes do not meet on the same banks; then the scales.
 template <int D>
 struct Tile4 {
   static constexpr int ROWB = D / 2, SROW = D / 32;
@@ -188,42 +188,103 @@ __device__ __forceinline__ float scale_at(uint32_t scales, int b) {
   return __uint_as_float(__builtin_amdgcn_alignbit(scales, scales, (8 * b + 9) & 31));
 }
 
-// A lane's pieces of two key rows 16 rows apart. Written by hand, because for one of the three
-// places the compiler waits for all copies in flight before it (64 contexts of 32k tokens:
-// 194 us, so 190).
+// What a lane holds of a tile: its pieces of the key rows of its operand row (dims (D/4) a4 ..)
+// and of the value rows of its slots (elements (D/16) n16 ..), and all these rows' scales
 template <int D>
-__device__ __forceinline__ void key_pieces(uint32_t (&u)[2][D / 32], const unsigned char* p) {
+struct Rows4 {
+  typedef unsigned pieces __attribute__((ext_vector_type(D / 32)));
+  typedef unsigned pair __attribute__((ext_vector_type(2)));
+  typedef unsigned quad __attribute__((ext_vector_type(4)));
+  pieces k[2];
+  pair ks;
+  uint32_t v[8];
+  quad vs[2];
+  // One wait for all of them. Written by hand, because the compiler has the reads of one of
+  // the three places wait for all copies in flight.
+  __device__ __forceinline__ void load(const unsigned char* kb, const unsigned char* vb, int a4, int n16) {
 #ifdef __HIP_DEVICE_COMPILE__
-  typedef unsigned uints __attribute__((ext_vector_type(D / 32)));
-  uints x, y;
-  const uint32_t at = (uint32_t)(uintptr_t)(lds_byte*)p;
-  if constexpr (D == 128)
-    asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %2 offset:1024\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x), "=&v"(y) : "v"(at) : "memory");
-  else
-    asm volatile("ds_read_b64 %0, %2\n\tds_read_b64 %1, %2 offset:512\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x), "=&v"(y) : "v"(at) : "memory");
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i) {
-    u[0][i] = x[i];
-    u[1][i] = y[i];
-  }
+    const int row = 4 * (n16 & 3) + (n16 >> 2);
+    const uint32_t at_k = (uint32_t)(uintptr_t)(lds_byte*)(kb + (D == 128 ? Tile4<D>::at(row, a4) : row * 32 + 8 * a4));
+    const uint32_t at_v = (uint32_t)(uintptr_t)(lds_byte*)(vb + a4 * Tile4<D>::ROWB + (D / 32) * n16);
+    const uint32_t at_ks = (uint32_t)(uintptr_t)(lds_byte*)(vb + Tile4<D>::BYTES + 4 * n16);
+    const uint32_t at_vs = (uint32_t)(uintptr_t)(lds_byte*)(vb + Tile4<D>::BYTES + 128 + 16 * a4);
+    if constexpr (D == 128) {
+      pair v0, v1, v2, v3;
+      asm volatile(
+          "ds_read_b128 %0, %9\n\t"
+          "ds_read_b128 %1, %9 offset:1024\n\t"
+          "ds_read2_b32 %2, %11 offset1:16\n\t"
+          "ds_read2st64_b32 %3, %10 offset0:0 offset1:4\n\t"
+          "ds_read2st64_b32 %4, %10 offset0:1 offset1:5\n\t"
+          "ds_read2st64_b32 %5, %10 offset0:2 offset1:6\n\t"
+          "ds_read2st64_b32 %6, %10 offset0:3 offset1:7\n\t"
+          "ds_read_b128 %7, %12\n\t"
+          "ds_read_b128 %8, %12 offset:64\n\t"
+          "s_waitcnt lgkmcnt(0)"
+          : "=&v"(k[0]), "=&v"(k[1]), "=&v"(ks), "=&v"(v0), "=&v"(v1), "=&v"(v2), "=&v"(v3), "=&v"(vs[0]), "=&v"(vs[1])
+          : "v"(at_k), "v"(at_v), "v"(at_ks), "v"(at_vs)
+          : "memory");
+      v[0] = v0[0];
+      v[4] = v0[1];
+      v[1] = v1[0];
+      v[5] = v1[1];
+      v[2] = v2[0];
+      v[6] = v2[1];
+      v[3] = v3[0];
+      v[7] = v3[1];
+    } else {
+      asm volatile(
+          "ds_read_b64 %0, %13\n\t"
+          "ds_read_b64 %1, %13 offset:512\n\t"
+          "ds_read2_b32 %2, %15 offset1:16\n\t"
+          "ds_read_u16 %3, %14\n\t"
+          "ds_read_u16 %4, %14 offset:128\n\t"
+          "ds_read_u16 %5, %14 offset:256\n\t"
+          "ds_read_u16 %6, %14 offset:384\n\t"
+          "ds_read_u16 %7, %14 offset:512\n\t"
+          "ds_read_u16 %8, %14 offset:640\n\t"
+          "ds_read_u16 %9, %14 offset:768\n\t"
+          "ds_read_u16 %10, %14 offset:896\n\t"
+          "ds_read_b128 %11, %16\n\t"
+          "ds_read_b128 %12, %16 offset:64\n\t"
+          "s_waitcnt lgkmcnt(0)"
+          : "=&v"(k[0]), "=&v"(k[1]), "=&v"(ks), "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]),
+            "=&v"(v[6]), "=&v"(v[7]), "=&v"(vs[0]), "=&v"(vs[1])
+          : "v"(at_k), "v"(at_v), "v"(at_ks), "v"(at_vs)
+          : "memory");
+    }
 #endif
-}
+  }
+  // a value row's scale (a lane's elements lie in one block of 32)
+  __device__ __forceinline__ float value_scale(int i, int n16) const { return scale_at(vs[i >> 2][i & 3], D == 128 ? n16 >> 2 : n16 >> 3); }
+  // Tiles where some query does not see some row: blocks of NaN would reach the outputs of
+  // the queries that do not see them as 0 NaN. They are taken out (bit i of the result: this
+  // lane's block of row i is one), ...
+  __device__ __forceinline__ unsigned take_nan(int n16) {
+    unsigned bad = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bool b = (__float_as_uint(value_scale(i, n16)) & 0x7f800000u) == 0x7f800000u;
+      bad |= b ? 1u << i : 0u;
+      v[i] = b ? 0u : v[i];
+      vs[i >> 2][i & 3] = b ? 0x7f7f7f7fu : vs[i >> 2][i & 3];  // (all of this lane's copy: 2^0)
+    }
+    return bad;
+  }
+};
 
 template <int D, int N>
-__device__ __forceinline__ void scores(float (&z)[8], const unsigned char* kb, const uint32_t* ks, const bf16x8 (&q)[N][D / 32],
-                                       int a4, int n16) {
-  const uint32_t byte[2] = {ks[n16], ks[16 + n16]};
-  uint32_t u[2][D / 32];
-  const int row = 4 * (n16 & 3) + (n16 >> 2);
-  key_pieces<D>(u, kb + (D == 128 ? Tile4<D>::at(row, a4) : row * 32 + 8 * a4));
+__device__ __forceinline__ void scores(float (&z)[8], const Rows4<D>& t, const bf16x8 (&q)[N][D / 32], int a4) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const float scale = scale_at(byte[h], D == 128 ? a4 : a4 >> 1);
+    const float scale = scale_at(t.ks[h], D == 128 ? a4 : a4 >> 1);
     f32x4 c = {0.f, 0.f, 0.f, 0.f};
     bf16x8 k[D / 32];
 #pragma unroll
-    for (int s = 0; s < D / 32; ++s)
-      k[s] = __builtin_bit_cast(bf16x8, make_uint4(two_of<0>(u[h][s], scale), two_of<1>(u[h][s], scale), two_of<2>(u[h][s], scale), two_of<3>(u[h][s], scale)));
+    for (int s = 0; s < D / 32; ++s) {
+      const uint32_t u = t.k[h][s];
+      k[s] = __builtin_bit_cast(bf16x8, make_uint4(two_of<0>(u, scale), two_of<1>(u, scale), two_of<2>(u, scale), two_of<3>(u, scale)));
+    }
 #pragma unroll
     for (int p = N - 1; p >= 0; --p)
 #pragma unroll
@@ -232,44 +293,6 @@ __device__ __forceinline__ void scores(float (&z)[8], const unsigned char* kb, c
     for (int r = 0; r < 4; ++r) z[4 * h + r] = c[r];
   }
 }
-
-// what a lane holds of a tile's values: the rows of its slots, elements (D/16) n16 ..
-template <int D>
-struct ValueRows {
-  uint32_t v[8];
-  float scale[8];
-  __device__ __forceinline__ void load(const unsigned char* vb, const uint32_t* vs, int a4, int n16) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int row = slot_row(a4, i);
-      if constexpr (D == 128) v[i] = *reinterpret_cast<const uint32_t*>(vb + row * 64 + 16 * ((n16 >> 2) ^ (i & 3)) + 4 * (n16 & 3));
-      else v[i] = *reinterpret_cast<const uint16_t*>(vb + row * 32 + 2 * n16);
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint4 x = *reinterpret_cast<const uint4*>(vs + 16 * h + 4 * a4);
-      const int b = D == 128 ? n16 >> 2 : n16 >> 3;  // (a lane's elements lie in one block of 32)
-      scale[4 * h] = scale_at(x.x, b);
-      scale[4 * h + 1] = scale_at(x.y, b);
-      scale[4 * h + 2] = scale_at(x.z, b);
-      scale[4 * h + 3] = scale_at(x.w, b);
-    }
-  }
-  // Tiles where some query does not see some row: blocks of NaN would reach the outputs of
-  // the queries that do not see them as 0 NaN. They are taken out (bit i of the result: this
-  // lane's block of row i is one), ...
-  __device__ __forceinline__ unsigned take_nan() {
-    unsigned bad = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const bool b = (__float_as_uint(scale[i]) & 0x7f800000u) == 0x7f800000u;
-      bad |= b ? 1u << i : 0u;
-      v[i] = b ? 0u : v[i];
-      scale[i] = b ? 1.f : scale[i];
-    }
-    return bad;
-  }
-};
 
 // The value product. The weights enter as the sum of three bf16 numbers, all 24 bits of
 // them (truncated one after another: exact).
@@ -290,13 +313,13 @@ struct Values {
     return p - __uint_as_float(__float_as_uint(p) & 0xffff0000u);
   }
   template <int B>
-  __device__ __forceinline__ void byte(const ValueRows<D>& t, const bf16x8 (&w)[FOLD ? 6 : 3]) {
+  __device__ __forceinline__ void byte(const Rows4<D>& t, const float (&scale)[8], const bf16x8 (&w)[FOLD ? 6 : 3]) {
     if constexpr (FOLD) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         uint32_t x[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = two_of<B>(t.v[4 * h + j], t.scale[4 * h + j]);
+        for (int j = 0; j < 4; ++j) x[j] = two_of<B>(t.v[4 * h + j], scale[4 * h + j]);
         const bf16x8 a = __builtin_bit_cast(bf16x8, make_uint4(x[0], x[1], x[2], x[3]));
 #pragma unroll
         for (int i = 0; i < 3; ++i) acc[B] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[3 * h + i], acc[B], 0, 0, 0);
@@ -305,7 +328,7 @@ struct Values {
       uint32_t lo[4], hi[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint32_t x = two_of<B>(t.v[2 * j], t.scale[2 * j]), y = two_of<B>(t.v[2 * j + 1], t.scale[2 * j + 1]);
+        const uint32_t x = two_of<B>(t.v[2 * j], scale[2 * j]), y = two_of<B>(t.v[2 * j + 1], scale[2 * j + 1]);
         lo[j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
         hi[j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
       }
@@ -319,7 +342,7 @@ struct Values {
     }
   }
   // p: the weights of the lane's rows
-  __device__ __forceinline__ void add(const ValueRows<D>& t, const float (&p)[8], int n16) {
+  __device__ __forceinline__ void add(const Rows4<D>& t, const float (&p)[8], int n16) {
     bf16x8 w[FOLD ? 6 : 3];
     float x[8];
 #pragma unroll
@@ -342,14 +365,17 @@ struct Values {
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = rest(x[i]);
     }
-    byte<0>(t, w);
-    byte<1>(t, w);
+    float scale[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) scale[i] = t.value_scale(i, n16);
+    byte<0>(t, scale, w);
+    byte<1>(t, scale, w);
     if constexpr (D == 128) {
-      byte<2>(t, w);
-      byte<3>(t, w);
+      byte<2>(t, scale, w);
+      byte<3>(t, scale, w);
     }
   }
-  // ... (ValueRows::take_nan) and the queries that do see one get NaN: by the number of such rows, a product of
+  // ... (Rows4::take_nan) and the queries that do see one get NaN: by the number of such rows, a product of
   // zeros and ones
   __device__ __forceinline__ void put_nan(unsigned bad, unsigned seen) {
     f32x4 count = {0.f, 0.f, 0.f, 0.f};
@@ -460,13 +486,12 @@ kv4_kernel(const WindowArgs a, const Kv4Cache four) {
   // rows by the others.
   const int copy_row = lane / (Q::ROWB / 16);
   const int copy_piece = (Q::at(copy_row, lane % (Q::ROWB / 16)) - copy_row * Q::ROWB) / 16;
-  const uint32_t copy_off = copy_row * Q::ROWB + 16 * copy_piece;
+  const uint32_t key_off = copy_row * Q::ROWB + 16 * copy_piece, value_off = 16 * lane;
   const int scale_row = scale_place(lane & 31);  // (its own inverse)
   const uint8_t* const scale_src = (lane < 32 ? four.ks : four.vs) + seq_s;
   auto copy = [&](const uint8_t* src, unsigned char* dst) {
     __builtin_amdgcn_global_load_lds((global_void*)src, (lds_void*)(lds_byte*)dst, 16, 0, kCopyPolicy);
   };
-  auto scales_at = [&](unsigned char* vb) { return reinterpret_cast<const uint32_t*>(vb + Q::BYTES); };
   auto copy_scales = [&](const uint8_t* src, unsigned char* dst) {
     __builtin_amdgcn_global_load_lds((global_void*)src, (lds_void*)(lds_byte*)dst, Q::SROW, 0, kCopyPolicy);
   };
@@ -487,12 +512,12 @@ kv4_kernel(const WindowArgs a, const Kv4Cache four) {
       const int r0 = t0 & bmask, r1 = (t0 + 16) & bmask;
       const int64_t c0 = blk.x * four.cb + static_cast<int64_t>(r0) * Q::ROWB, c1 = blk.y * four.cb + static_cast<int64_t>(r1) * Q::ROWB;
       if constexpr (D == 128) {
-        copy(Kc + c0 + copy_off, kb);
-        copy(Kc + c1 + copy_off, kb + 1024);
-        copy(Vc + c0 + copy_off, vb);
-        copy(Vc + c1 + copy_off, vb + 1024);
+        copy(Kc + c0 + key_off, kb);
+        copy(Kc + c1 + key_off, kb + 1024);
+        copy(Vc + c0 + value_off, vb);
+        copy(Vc + c1 + value_off, vb + 1024);
       } else {
-        const int64_t c = (lane < 32 ? c0 : c1 - 16 * Q::ROWB) + copy_off;
+        const int64_t c = (lane < 32 ? c0 : c1 - 16 * Q::ROWB) + value_off;
         copy(Kc + c, kb);
         copy(Vc + c, vb);
       }
@@ -501,9 +526,9 @@ kv4_kernel(const WindowArgs a, const Kv4Cache four) {
     } else {
       const int64_t c = static_cast<int64_t>(t0) * Q::ROWB;
 #pragma unroll
-      for (int j = 0; j < Q::COPIES; ++j) copy(Kc + c + (copy_off + 1024 * j), kb + 1024 * j);
+      for (int j = 0; j < Q::COPIES; ++j) copy(Kc + c + (key_off + 1024 * j), kb + 1024 * j);
 #pragma unroll
-      for (int j = 0; j < Q::COPIES; ++j) copy(Vc + c + (copy_off + 1024 * j), vb + 1024 * j);
+      for (int j = 0; j < Q::COPIES; ++j) copy(Vc + c + (value_off + 1024 * j), vb + 1024 * j);
       copy_scales(scale_src + static_cast<int64_t>(t0) * Q::SROW + scale_row * Q::SROW, vb + Q::BYTES);
     }
   };
@@ -521,9 +546,9 @@ kv4_kernel(const WindowArgs a, const Kv4Cache four) {
 #pragma unroll
     for (int j = 0; j < Q::COPIES; ++j) {
       const int row = place(1024 / Q::ROWB * j + copy_row, block);
-      const int64_t c = block * four.cb + static_cast<int64_t>(row) * Q::ROWB + 16 * copy_piece;
-      copy(Kc + c, kb + 1024 * j);
-      copy(Vc + c, vb + 1024 * j);
+      const int64_t c = block * four.cb + static_cast<int64_t>(row) * Q::ROWB;
+      copy(Kc + c + 16 * copy_piece, kb + 1024 * j);
+      copy(Vc + c + 16 * (lane % (Q::ROWB / 16)), vb + 1024 * j);
     }
     const int row = place(scale_row, block);
     copy_scales(scale_src + block * four.sb + static_cast<int64_t>(row) * Q::SROW, vb + Q::BYTES);
@@ -573,8 +598,10 @@ kv4_kernel(const WindowArgs a, const Kv4Cache four) {
     __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
     request_any(k, k2, v2);
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    Rows4<D> rows;
+    rows.load(k2, v2, a4, n16);
     float z[8];
-    scores<D>(z, k2, scales_at(v2), q.v, a4, n16);
+    scores<D>(z, rows, q.v, a4);
     unsigned seen = 0xffu;
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
@@ -585,9 +612,7 @@ kv4_kernel(const WindowArgs a, const Kv4Cache four) {
       }
     }
     weigh(z);
-    ValueRows<D> rows;
-    rows.load(v2, scales_at(v2) + 32, a4, n16);
-    const unsigned bad = rows.take_nan();
+    const unsigned bad = rows.take_nan(n16);
     out.add(rows, z, n16);
     if (__builtin_amdgcn_ballot_w64(bad != 0)) out.put_nan(bad, seen);
   }
@@ -606,11 +631,11 @@ kv4_kernel(const WindowArgs a, const Kv4Cache four) {
     } else {
       __builtin_amdgcn_s_waitcnt(kWaitVm0);
     }
+    Rows4<D> rows;
+    rows.load(kb, vb, a4, n16);
     float z[8];
-    scores<D>(z, kb, scales_at(vb), q.v, a4, n16);
+    scores<D>(z, rows, q.v, a4);
     weigh(z);
-    ValueRows<D> rows;
-    rows.load(vb, scales_at(vb) + 32, a4, n16);
     out.add(rows, z, n16);
     i += kWinWaves;
   };
