@@ -177,6 +177,7 @@ __global__ __launch_bounds__(64 * kAppendWaves) void append_kernel(const AppendA
   constexpr int ESZ = DT == VP_BF16 ? 2 : 4;
   constexpr int LANES = D / 8;      // lanes of a row
   constexpr int ROWS = 64 / LANES;  // rows of a wave
+  constexpr int BATCH = 3;  // rows of a lane whose loads are in flight together
   const int lane = threadIdx.x & 63;
   const int64_t id = static_cast<int64_t>(blockIdx.x) * kAppendWaves + __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   if (id >= static_cast<int64_t>(a.n_tokens) * a.waves) return;
@@ -217,47 +218,56 @@ __global__ __launch_bounds__(64 * kAppendWaves) void append_kernel(const AppendA
 
   const int Hq = a.q ? a.Hq : 0;
   const int rows = Hq + 2 * a.Hkv;
-  for (int r = first + lane / LANES; r < rows; r += a.waves * ROWS) {
-    const int h = r < Hq ? r : r < Hq + a.Hkv ? r - Hq : r - Hq - a.Hkv;
-    const char* src;
-    if (r < Hq) src = static_cast<const char*>(a.q) + token * a.qs;
-    else if (r < Hq + a.Hkv) src = static_cast<const char*>(a.k) + token * a.ks;
-    else src = static_cast<const char*>(a.v) + token * a.vs;
-    src += h * (D * ESZ);
-    const bool value = r >= Hq + a.Hkv;
-    const bool turn_it = turns && !value;
-    Octet<DT> x, y;
-    x.load(src + octet * (8 * ESZ));
-    y = x;
-    if (turn_it) y.load(src + partner * (8 * ESZ));
-    if (FOUR && r >= Hq) {
-      float f[8];
+  const int step = a.waves * ROWS;
+  const char* const qs = static_cast<const char*>(a.q) + token * a.qs;
+  const char* const ks = static_cast<const char*>(a.k) + token * a.ks;
+  const char* const vs = static_cast<const char*>(a.v) + token * a.vs;
+  for (int r0 = first + lane / LANES; r0 - lane / LANES < rows; r0 += BATCH * step) {
+    Octet<DT> x[BATCH], y[BATCH];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = turn_it ? to_odd(turned<DT>(a, turn, x, y, upper, j)) : x.get(j);
-      uint32_t byte;
-      const uint32_t codes = to_4bit(f, byte);
-      // the row's scales meet in its first lane
-      uint32_t all = byte << 8 * (octet >> 2);
-      all |= static_cast<uint32_t>(__shfl_xor(static_cast<int>(all), 4));
-      if constexpr (D == 128) all |= static_cast<uint32_t>(__shfl_xor(static_cast<int>(all), 8));
-      uint8_t* cd = (value ? a.four.vc : a.four.kc) + at * a.four.cb + h * a.four.ch + static_cast<int64_t>(in) * (D / 2);
-      uint8_t* sd = (value ? a.four.vs : a.four.ks) + at * a.four.sb + h * a.four.sh + static_cast<int64_t>(in) * (D / 32);
-      reinterpret_cast<uint32_t*>(cd)[octet] = codes;
-      if (octet == 0) {
-        if constexpr (D == 128) *reinterpret_cast<uint32_t*>(sd) = all;
-        else *reinterpret_cast<uint16_t*>(sd) = static_cast<uint16_t>(all);
-      }
-    } else {
-      if (turn_it) {
+    for (int j = 0; j < BATCH; ++j) {
+      const int r = min(r0 + j * step, rows - 1);
+      const bool key = r < Hq + a.Hkv;
+      const char* src = r < Hq ? qs + r * (D * ESZ) : key ? ks + (r - Hq) * (D * ESZ) : vs + (r - Hq - a.Hkv) * (D * ESZ);
+      x[j].load(src + octet * (8 * ESZ));
+      y[j].load(src + (key ? partner : octet) * (8 * ESZ));
+    }
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+      const int r = r0 + j * step;
+      if (r >= rows) break;
+      const bool value = r >= Hq + a.Hkv;
+      const int h = r < Hq ? r : value ? r - Hq - a.Hkv : r - Hq;
+      const bool turn_it = turns && !value;
+      if (FOUR && r >= Hq) {
         float f[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = static_cast<float>(turned<DT>(a, turn, x, y, upper, j));
-        x.set(f);
+        for (int i = 0; i < 8; ++i) f[i] = turn_it ? to_odd(turned<DT>(a, turn, x[j], y[j], upper, i)) : x[j].get(i);
+        uint32_t byte;
+        const uint32_t codes = to_4bit(f, byte);
+        // the row's scales meet in its first lane
+        uint32_t all = byte << 8 * (octet >> 2);
+        all |= static_cast<uint32_t>(__shfl_xor(static_cast<int>(all), 4));
+        if constexpr (D == 128) all |= static_cast<uint32_t>(__shfl_xor(static_cast<int>(all), 8));
+        uint8_t* cd = (value ? a.four.vc : a.four.kc) + at * a.four.cb + h * a.four.ch + static_cast<int64_t>(in) * (D / 2);
+        uint8_t* sd = (value ? a.four.vs : a.four.ks) + at * a.four.sb + h * a.four.sh + static_cast<int64_t>(in) * (D / 32);
+        reinterpret_cast<uint32_t*>(cd)[octet] = codes;
+        if (octet == 0) {
+          if constexpr (D == 128) *reinterpret_cast<uint32_t*>(sd) = all;
+          else *reinterpret_cast<uint16_t*>(sd) = static_cast<uint16_t>(all);
+        }
+      } else {
+        if (turn_it) {
+          float f[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) f[i] = static_cast<float>(turned<DT>(a, turn, x[j], y[j], upper, i));
+          x[j].set(f);
+        }
+        char* dst;
+        if (r < Hq) dst = static_cast<char*>(a.q_out) + (static_cast<int64_t>(token) * Hq + h) * (D * ESZ);
+        else dst = static_cast<char*>(value ? a.V : a.K) + at * a.sb + h * a.sh + in * a.ss;
+        x[j].store(dst + octet * (8 * ESZ));
       }
-      char* dst;
-      if (r < Hq) dst = static_cast<char*>(a.q_out) + (static_cast<int64_t>(token) * Hq + h) * (D * ESZ);
-      else dst = static_cast<char*>(value ? a.V : a.K) + at * a.sb + h * a.sh + in * a.ss;
-      x.store(dst + octet * (8 * ESZ));
     }
   }
 }
@@ -277,7 +287,7 @@ hipError_t launch_append(const AppendArgs& in, bool four, int dtype, int head_di
   AppendArgs a = in;
   if (a.n_tokens == 0) return hipSuccess;
   const int batches = ((a.q ? a.Hq : 0) + 2 * a.Hkv + 512 / head_dim - 1) / (512 / head_dim);
-  a.waves = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(batches, 8192 / a.n_tokens)));
+  a.waves = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(batches, std::max<int64_t>(8192 / a.n_tokens, batches / 6))));
   if (dtype == VP_BF16) return head_dim == 128 ? launch_dd<VP_BF16, 128>(a, four, st) : launch_dd<VP_BF16, 64>(a, four, st);
   return head_dim == 128 ? launch_dd<VP_F32, 128>(a, four, st) : launch_dd<VP_F32, 64>(a, four, st);
 }

@@ -96,10 +96,13 @@ __global__ __launch_bounds__(kReadThreads) void read_kernel(const ReadArgs a) {
 
 template <int DT, int D>
 hipError_t read_dd(const ReadArgs& a, hipStream_t st) {
-  // (a capacity far above the lengths costs no more work-groups than a full GPU needs)
+  // Work-groups enough to fill the GPU many times over where whole contexts are read (16 of 5k
+  // to 12k rows, 4 KV heads: 72 us, with a quarter of them 77, with a sixteenth 84). Where `first`
+  // leaves a few rows of each they find nothing to do: fewer then (64 sequences, 2 rows each: 5 us
+  // and 8 with four times as many).
   const int64_t per = 4 * (kReadThreads / (D / 8));
   const int64_t pairs = static_cast<int64_t>(a.B) * a.Hkv * 2;
-  const int64_t chunks = std::min((a.max_seq_len + per - 1) / per, std::max<int64_t>(1, 8192 / pairs));
+  const int64_t chunks = std::min((a.max_seq_len + per - 1) / per, std::max<int64_t>(1, (a.first ? 2048 : 32768) / pairs));
   for (int b0 = 0; b0 < a.B; b0 += 32767) {  // (the grid's third dimension ends at 65535)
     ReadArgs x = a;
     x.B = std::min(32767, a.B - b0);
