@@ -728,10 +728,25 @@ WindowPlan make_kv4_plan(const vp_shape& s, const vp_window& w) {
   const int64_t cap = (static_cast<int64_t>(s.max_seq_len) + 31) / 32;
   const int64_t tiles = p.tiles = window_tiles(s, w);
   const int64_t pairs = static_cast<int64_t>(s.batch) * s.n_kv_heads;
+  // One work-group per pair, and no second launch, as make_window_plan has it (a tile takes
+  // half as long here: 0.16 us), where (us whole and dealt; bf16, d = 128)
+  // * the walks are short: up to 28 tiles (4 KV heads; 1 sequence: 16 tiles 7.1 and 9.4, 32
+  //   tiles 10.0 and 9.5; 16 sequences: 16 tiles 7.4 and 9.9, 32 tiles 10.5 and 11.1, 64 tiles
+  //   15.8 and 13.4);
+  // * the longest walk is short beside what dealing costs (64 sequences, 256 pairs: 16 tiles
+  //   8.3 and 15.4, 32 tiles 11.1 and 17.9, 128 tiles 29.2 and 34.7, lengths from a tenth of
+  //   that 27.8 and 27.8, 256 tiles 55.6 and 57.1, 48.1 and 41.2; 128 sequences, 64 tiles 28.8
+  //   and 37.7);
+  // * a window cuts the walks of the capacity to half or less, and the pairs nearly fill the
+  //   CUs (as above: equal walks).
+  const bool brief = 1200 * tiles <= pairs * (350 + s.batch);
   const bool cut = w.window > 0 && 2 * tiles <= cap;
-  const bool brief = 2400 * tiles <= pairs * (350 + s.batch);
-  const bool one_each = tiles <= 16 || brief || (cut && pairs >= 512) || pairs * tiles > 0x3fffffff;
-  const int64_t most = std::max<int64_t>(512, 2 * pairs);
+  const bool one_each = tiles <= 28 || brief || (cut && pairs >= 192) || pairs * tiles > 0x3fffffff;
+  // Otherwise two work-groups per CU (three or four, where registers allow them: 64 x 32k
+  // 190 and 190, 16 x 12k ragged 21.3 and 22.3 to 24.2), twice as many as pairs where those are
+  // more, a tile per wave at least; and no more than 32 for a walk, whose pieces the second
+  // launch joins (1 sequence of 8k: 11.0 and, 64 each, 12.1; of 32k 14.9 and, 128 each, 19.2)
+  const int64_t most = std::min<int64_t>(std::max<int64_t>(512, 2 * pairs), 32 * pairs);
   p.groups = one_each ? 0 : static_cast<int>(std::min(most, pairs * ((tiles + kWinWaves - 1) / kWinWaves)));
   carve_window_plan(p, s, false);
   return p;
