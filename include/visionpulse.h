@@ -480,7 +480,7 @@ typedef struct vp_tokens {
   int64_t v_stride;
   const int32_t* new_off;  /* device [B+1], ascending: sequence b has tokens new_off[b] .. new_off[b+1] - 1;
                               NULL: n_queries tokens each */
-  int32_t n_tokens;        /* rows of q, k, v (those that new_off gives to no sequence are left alone) */
+  int32_t n_tokens;        /* rows of q, k, v, at most 2^24 (those that new_off gives to no sequence are left alone) */
 } vp_tokens;
 
 /* A 4-bit cache. A row of d elements is d/2 bytes of codes, two elements a byte, the

@@ -67,6 +67,7 @@ vp_status static_scratch(void** ptr) {
 constexpr int kMaxGroup = 16;
 constexpr int kMaxHq = kMaxHq_;
 constexpr int kMaxBatch = 65535;
+constexpr int kMaxNewTokens = 1 << 24;  // tokens that a call appends (a wave or more each)
 constexpr int kMaxTokens = 1 << 28;  // bound on max_seq_len, max_vis and k_cap (32-bit index arithmetic)
 
 
@@ -421,6 +422,11 @@ vp_status check_rope(const vp_shape* s, const vp_rope* r) {
 
 vp_status check_tokens(const vp_shape* s, const vp_tokens* t, const void* q_out) {
   if (!t) return fail(VP_ERR_NULL, "tokens is NULL");
+  if (t->n_tokens < 0 || t->n_tokens > kMaxNewTokens)
+    return fail(VP_ERR_RANGE, "n_tokens %d outside [0, %d]", t->n_tokens, kMaxNewTokens);
+  if (!t->new_off && t->n_tokens != static_cast<int64_t>(s->batch) * queries(*s))
+    return fail(VP_ERR_SHAPE, "n_tokens %d without new_off: batch %d x n_queries %d", t->n_tokens, s->batch, queries(*s));
+  if (t->n_tokens == 0) return VP_OK;  // (nothing is read)
   if (!t->k || !t->v) return fail(VP_ERR_NULL, "tokens k and v required");
   if (!t->q != !q_out) return fail(VP_ERR_NULL, "q and q_out: both or neither");
   if (!aligned16(t->q) || !aligned16(t->k) || !aligned16(t->v) || !aligned16(q_out))
@@ -434,9 +440,6 @@ vp_status check_tokens(const vp_shape* s, const vp_tokens* t, const void* q_out)
     return fail(VP_ERR_SHAPE, "token strides must be multiples of %lld elements (16 bytes)", (long long)step);
   if (t->q && t->q == q_out && t->q_stride != qw) return fail(VP_ERR_SHAPE, "q_out is q, whose tokens are not next to each other");
   if (reinterpret_cast<uintptr_t>(t->new_off) & 3u) return fail(VP_ERR_SHAPE, "new_off must be 4-byte aligned");
-  if (t->n_tokens < 0 || t->n_tokens > kMaxTokens) return fail(VP_ERR_RANGE, "n_tokens %d outside [0, %d]", t->n_tokens, kMaxTokens);
-  if (!t->new_off && t->n_tokens != static_cast<int64_t>(s->batch) * queries(*s))
-    return fail(VP_ERR_SHAPE, "n_tokens %d without new_off: batch %d x n_queries %d", t->n_tokens, s->batch, queries(*s));
   return VP_OK;
 }
 
@@ -455,7 +458,7 @@ vp_status check_kv4(const vp_shape* s, const vp_kv4* c, bool written) {
     return fail(VP_ERR_SHAPE, "strides of 4-bit caches must be multiples of 16 bytes");
   if (!written) return VP_OK;
   if (c->k_codes == c->v_codes || c->k_scales == c->v_scales) return fail(VP_ERR_SHAPE, "K and V are the same cache");
-  const int64_t rows = s->block_size > 0 ? s->block_size : s->max_seq_len;
+  const int64_t rows = s->block_size > 0 ? std::min(s->block_size, s->max_seq_len) : s->max_seq_len;
   const int64_t count_b = s->block_size > 0 ? 2 : s->batch;  // (blocks: any two)
   auto apart = [&](int64_t sb, int64_t sh, int64_t row_bytes) {
     int64_t small = sh, n = s->n_kv_heads, large = sb, m = count_b;

@@ -1,5 +1,6 @@
-"""Device buffers for one decode step and the four C-ABI calls in order, and the
-calls of a bounded cache (window attention, eviction) on the same buffers.
+"""Device buffers for one decode step and the four C-ABI calls in order, and on the
+same buffers the calls of a bounded cache (window attention, eviction), those that
+append tokens, and those of a 4-bit cache.
 
 Marshalling only: uploads a ``workloads.Workload`` to the GPU (torch
 allocations), fills the ABI structs and calls vp_visual_mass -> vp_budget ->
@@ -47,6 +48,26 @@ def paged_cache(K: np.ndarray, V: np.ndarray, block_size: int, seed: int = 0):
             Kp[table[b, j], :, :r1 - r0] = K[b, :, r0:r1]
             Vp[table[b, j], :, :r1 - r0] = V[b, :, r0:r1]
     return Kp, Vp, np.ascontiguousarray(table)
+
+
+def make_rope(cos_sin: torch.Tensor, pos: torch.Tensor | None = None, sections=None, interleaved: bool = False) -> vp.vp_rope:
+    """Rotation by position for ``DeviceStep.append``: cos_sin float32 [n_pos, rot_dim] on the
+    device (cosines, then sines); pos int32 [n_tokens] or [n_axes, n_tokens] (None: cache rows);
+    sections: pairs of each axis. The tensors stay alive with the result."""
+    if cos_sin.dtype != torch.float32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous():
+        raise ValueError("make_rope: cos_sin must be a contiguous float32 [n_pos, rot_dim]")
+    if pos is not None and (pos.dtype != torch.int32 or not pos.is_contiguous() or pos.device != cos_sin.device):
+        raise ValueError("make_rope: pos must be a contiguous int32 tensor on cos_sin's device")
+    axes = len(sections) if sections else 1
+    if axes > 4:
+        raise ValueError(f"make_rope: {axes} axes, at most 4")
+    if pos is not None and (pos.shape[0] != axes if pos.dim() == 2 else axes > 1):
+        raise ValueError(f"make_rope: pos {tuple(pos.shape)} for {axes} axes")
+    sec = (ctypes.c_int32 * 4)(*[*(sections or ()), *[0] * (4 - len(sections or ()))])
+    r = vp.vp_rope(cos_sin=cos_sin.data_ptr(), n_pos=cos_sin.shape[0], rot_dim=cos_sin.shape[1],
+                   interleaved=int(interleaved), n_axes=axes, pos=None if pos is None else pos.data_ptr(), section=sec)
+    r.tensors = (cos_sin, pos)
+    return r
 
 
 class DeviceStep:
@@ -114,6 +135,7 @@ class DeviceStep:
         self.out = torch.zeros(B * T, Hq, d, dtype=self.q.dtype, device=self.device)
         self.attn_sum = None      # running attention weights (window_decode_attn)
         self._bounded_ws = []
+        self.kv4 = None           # the 4-bit cache (make_kv4)
         self.ws_bytes = vp.vp_workspace_size(self.shape)
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
 
@@ -196,6 +218,76 @@ class DeviceStep:
         vp.vp_evict(shape, self.layout, opt, self.attn_sum, self.K, self.V, kept, self.attn_sum,
                     None if groups else self.seg, self.seq_len, ws, nbytes, stream)
         return kept
+
+    # appending, and a cache of 4 bits ---------------------------------------
+    def make_kv4(self):
+        """A 4-bit cache for these sequences, of the same blocks where caches are paged: codes
+        and scales of K and V (``kv4_codes``, ``kv4_scales``), what lies in them unset."""
+        n, rows = self.K.shape[0], -(-self.K.shape[2] // 16) * 16
+        u8 = lambda width: [torch.empty(n, self.w.Hkv, rows, width, dtype=torch.uint8, device=self.device) for _ in range(2)]
+        self.kv4_codes, self.kv4_scales = u8(self.w.d // 2), u8(self.w.d // 32)
+        (kc, vc), (ks, vs) = self.kv4_codes, self.kv4_scales
+        self.kv4 = vp.vp_kv4(k_codes=kc.data_ptr(), k_scales=ks.data_ptr(), v_codes=vc.data_ptr(), v_scales=vs.data_ptr(),
+                             code_stride_b=kc.stride(0), code_stride_h=kc.stride(1), scale_stride_b=ks.stride(0),
+                             scale_stride_h=ks.stride(1))
+        return self.kv4
+
+    def _kv4(self, call):
+        if self.kv4 is None:
+            raise RuntimeError(f"{call}: no 4-bit cache yet (make_kv4 makes it)")
+        return self.kv4
+
+    def append(self, k, v, q=None, rope=None, new_off=None, q_out=None, four=False, stream=None):
+        """vp_append_kv, or with ``four`` vp_append_kv4 into the 4-bit cache: tokens k, v
+        [n, Hkv, d] and, if given, q [n, Hq, d] (slices of one product's columns will do) to the last
+        rows of their sequences, whose ``seq_len`` counts them already. new_off int32 [B+1]: how
+        many each sequence has (None: the step's queries each, n = B * T). Rotated queries go to
+        q_out (None: ``q``, the step's queries; n = B * T then). Returns q_out."""
+        n, d = k.shape[0], self.w.d
+        for name, x, heads in (("k", k, self.w.Hkv), ("v", v, self.w.Hkv), ("q", q, self.w.Hq)):
+            if x is None:
+                continue
+            if tuple(x.shape) != (n, heads, d) or x.dtype != self.q.dtype or x.device != self.K.device:
+                raise ValueError(f"append: {name} is {x.dtype} {tuple(x.shape)} on {x.device}, not {self.q.dtype} "
+                                 f"{(n, heads, d)} on {self.K.device}")
+            if n and (x.stride(2) != 1 or x.stride(1) != d):
+                raise ValueError(f"append: a token's heads in {name} must lie next to each other")
+        if new_off is not None and (new_off.dtype != torch.int32 or new_off.numel() != self.w.B + 1
+                                    or not new_off.is_contiguous() or new_off.device != self.K.device):
+            raise ValueError(f"append: new_off must be int32 [{self.w.B + 1}] on {self.K.device}")
+        pos = getattr(rope, "tensors", (None, None))[1]
+        if pos is not None and pos.shape[-1] != n:
+            raise ValueError(f"append: positions of {pos.shape[-1]} tokens for {n}")
+        if q is not None and q_out is None:
+            q_out = self.q
+        if q_out is not None and (q is None or q_out.numel() != n * self.w.Hq * d or q_out.dtype != self.q.dtype
+                                  or not q_out.is_contiguous()):
+            raise ValueError(f"append: q_out must be contiguous, with room for the {n} rotated queries")
+        step = lambda x, heads: x.stride(0) if n > 1 else heads * d  # (one token's stride means nothing)
+        tokens = vp.vp_tokens(q=None if q is None else q.data_ptr(), k=k.data_ptr(), v=v.data_ptr(),
+                              q_stride=0 if q is None else step(q, self.w.Hq), k_stride=step(k, self.w.Hkv),
+                              v_stride=step(v, self.w.Hkv), new_off=None if new_off is None else new_off.data_ptr(),
+                              n_tokens=n)
+        if four:
+            vp.vp_append_kv4(self.shape, self.layout, rope, tokens, q_out, self._kv4("append"), stream)
+        else:
+            vp.vp_append_kv(self.shape, self.layout, rope, tokens, q_out, self.K, self.V, stream)
+        return q_out
+
+    def kv4_decode_attn(self, window=0, n_sink=0, sm_scale=0.0, stream=None):
+        """vp_kv4_decode_attn into ``out``: window_decode_attn over the 4-bit cache."""
+        opt = vp.vp_window(window=window, n_sink=n_sink, sm_scale=sm_scale)
+        cache = self._kv4("kv4_decode_attn")
+        nbytes = vp.vp_kv4_workspace_size(self.shape, opt)
+        with self._order_of(stream):
+            ws = self._workspace(nbytes)
+        vp.vp_kv4_decode_attn(self.shape, self.layout, opt, self.q, cache, self.out, ws, nbytes, stream)
+
+    def kv4_read(self, first=None, stream=None):
+        """vp_kv4_read: the 4-bit cache's rows from first[b] on (int32 [B]; None: all) into K and V."""
+        if first is not None and (first.dtype != torch.int32 or first.numel() != self.w.B or not first.is_contiguous()):
+            raise ValueError(f"kv4_read: first must be int32 [{self.w.B}]")
+        vp.vp_kv4_read(self.shape, self.layout, self._kv4("kv4_read"), first, self.K, self.V, stream)
 
     def run(self, fused=True, stream=None):
         self.visual_mass(fused, stream)

@@ -267,6 +267,42 @@ def test_infinite_queries():
         assert bool((got[0, 0, 0] == 0).all()) and bool((got[0, 0, 1] == 1).all()), dtype
 
 
+@pytest.mark.parametrize("B,Hkv,cap,window", [(100, 1, 3000, 0), (70, 2, 2500, 1900), (300, 1, 700, 0), (260, 3, 300, 64)])
+def test_many_sequences(B, Hkv, cap, window):
+    """More sequences than a wave has lanes, dealt and whole."""
+    rng = np.random.default_rng(B)
+    lens = np.where(rng.random(B) < 0.1, cap, rng.integers(0, 40, B)).tolist()
+    c, qd, q, K, V = _case(rng, lens, 3 * Hkv, Hkv, 64, "bf16", 1, cap=cap, page=32)
+    _check(_attention(c, qd, lens, window, 3, "bf16"), q, K, V, window, 3, "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_heads(dtype):
+    rng = np.random.default_rng(12)
+    lens = [70, 33]
+    c, qd, q, K, V = _case(rng, lens, 512, 256, 64, dtype, 1)
+    _check(_attention(c, qd, lens, 0, 0, dtype), q, K, V, 0, 0, dtype)
+
+
+def test_heads_outside_sequences():
+    """Planes of a head before those of a sequence ([Hkv][B][rows]), and lengths outside the capacity."""
+    rng = np.random.default_rng(13)
+    B, Hkv, cap, d = 3, 2, 48, 128
+    c, qd, q, K, V = _case(rng, [48, 20, 0], 8, Hkv, d, "bf16", 1, cap=cap)
+    want = _attention(c, qd, [48, 20, 0], 0, 0, "bf16")
+    c.codes = [x.transpose(0, 1).contiguous().transpose(0, 1) for x in c.codes]
+    c.scales = [x.transpose(0, 1).contiguous().transpose(0, 1) for x in c.scales]
+    assert bool((_attention(c, qd, [60, 20, -5], 0, 0, "bf16") == want).all())
+    new = New(rng, 4, 8, Hkv, d, "bf16", queries=False)
+    seq_len, off = i32([48, 20, 9]), i32([0, 2, 2, 4])
+    vp.vp_append_kv4(c.shape(8, "bf16"), c.layout(seq_len), None, new.struct(off), None, c.struct())
+    Kg, Vg = c.get(cap)
+    for b, (lo, hi, i) in {0: (46, 48, 0), 2: (7, 9, 2)}.items():
+        assert np.array_equal(Kg[b][:, lo:hi], _held(new.k[i:i + 2].transpose(1, 0, 2)))
+        assert np.array_equal(Vg[b][:, lo:hi], _held(new.v[i:i + 2].transpose(1, 0, 2)))
+    assert np.array_equal(Kg[1][:, :20], K[1]) and np.array_equal(Kg[0][:, :46], K[0][:, :46])
+
+
 def test_far_offsets():
     """Planes beyond 2^32 bytes: a block far into a pool, and a sequence far into a batch."""
     rng = np.random.default_rng(9)

@@ -92,6 +92,7 @@ def test_rotation(call, status, kw):
     ("VP_ERR_SHAPE", dict(q=PTR + 8)), ("VP_ERR_SHAPE", dict(k=PTR + 2)), ("VP_ERR_SHAPE", dict(v=PTR + 4)),
     ("VP_ERR_SHAPE", dict(q_stride=28 * 128 - 8)), ("VP_ERR_SHAPE", dict(k_stride=0)), ("VP_ERR_SHAPE", dict(v_stride=-512)),
     ("VP_ERR_SHAPE", dict(k_stride=515)), ("VP_ERR_SHAPE", dict(new_off=PTR + 1)), ("VP_ERR_RANGE", dict(n_tokens=-1)),
+    ("VP_ERR_RANGE", dict(n_tokens=(1 << 24) + 1)), ("VP_ERR_SHAPE", dict(new_off=None, n_tokens=0)),
     ("VP_ERR_SHAPE", dict(new_off=None)),  # 5 tokens for 2 sequences of one query
 ])
 def test_tokens(call, status, kw):
@@ -107,6 +108,12 @@ def test_append_arguments(call):
     _refused("VP_ERR_SHAPE", call, None, None, None, None, PTR)  # q_out is q, a column of one product
     _refused("VP_ERR_DTYPE", call, _shape(dtype=4))
     _refused("VP_ERR_UNSUPPORTED", call, _shape(head_dim=96))
+
+
+@pytest.mark.parametrize("call", [_append, _append4])
+def test_no_tokens(call):
+    """Nothing to append: nothing is enqueued, and empty tensors' addresses do not matter."""
+    call(None, None, _rope(), _tokens(n_tokens=0, k=None, v=None, q=None), None)
 
 
 def test_append_caches():
