@@ -128,27 +128,32 @@ hipError_t read_dd(const ReadArgs& a, hipStream_t st) {
 // vp_kv4_decode_attn
 // ---------------------------------------------------------------------------
 
-// query rows as bf16 operands: slot (a4, i) of step s <-> dim (D/4) a4 + 8 s + i
+// query rows as bf16 operands: slot (a4, i) of step s <-> dim (D/4) a4 + 8 s + i. fp32 rows
+// are fetched first and taken apart once the first tiles are requested.
 template <int DT, int D>
 struct Queries {
   static constexpr int N = DT == VP_BF16 ? 1 : 3;
   bf16x8 v[N][D / 32];
-  __device__ __forceinline__ void load(const char* row, bool valid, int a4) {
+  float4 raw[DT == VP_BF16 ? 1 : D / 16];
+  __device__ __forceinline__ void fetch(const char* row, bool valid, int a4) {
+    if constexpr (DT == VP_BF16) {
 #pragma unroll
-    for (int s = 0; s < D / 32; ++s) {
-      if constexpr (DT == VP_BF16) {
+      for (int s = 0; s < D / 32; ++s) {
         const uint4 u = valid ? reinterpret_cast<const uint4*>(row)[(D / 32) * a4 + s] : make_uint4(0, 0, 0, 0);
         v[0][s] = __builtin_bit_cast(bf16x8, u);
-      } else {
-        float x[8];
+      }
+    } else {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float4 u = valid ? reinterpret_cast<const float4*>(row)[2 * ((D / 32) * a4 + s) + i] : make_float4(0.f, 0.f, 0.f, 0.f);
-          x[4 * i] = u.x;
-          x[4 * i + 1] = u.y;
-          x[4 * i + 2] = u.z;
-          x[4 * i + 3] = u.w;
-        }
+      for (int s = 0; s < D / 16; ++s)
+        raw[s] = valid ? reinterpret_cast<const float4*>(row)[(D / 16) * a4 + s] : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+  }
+  __device__ __forceinline__ void split() {
+    if constexpr (DT == VP_F32) {
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) {
+        const float x[8] = {raw[2 * s].x,     raw[2 * s].y,     raw[2 * s].z,     raw[2 * s].w,
+                            raw[2 * s + 1].x, raw[2 * s + 1].y, raw[2 * s + 1].z, raw[2 * s + 1].w};
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           // (an infinity leaves no rest)
@@ -466,7 +471,7 @@ kv4_kernel(const WindowArgs a, const Kv4Cache four) {
   }
   // the query rows load while the length arrives
   Queries<DT, D> q;
-  q.load(static_cast<const char*>(a.q) + (hv ? out_row(a, b, g, col) : 0) * (D * (DT == VP_BF16 ? 2 : 4)), hv, a4);
+  q.fetch(static_cast<const char*>(a.q) + (hv ? out_row(a, b, g, col) : 0) * (D * (DT == VP_BF16 ? 2 : 4)), hv, a4);
   const WindowWalk w(L, a.T, a.window, a.n_sink);
   const int hi = w.L - a.T + tq;                        // this lane's query sees j <= hi
   const int below = a.window > 0 ? hi - a.window : -1;  // and j > below or j < n_sink
@@ -584,8 +589,10 @@ kv4_kernel(const WindowArgs a, const Kv4Cache four) {
   };
 
   // this part's run of inner tiles, and this wave's first one
-  int i = static_cast<int>(static_cast<int64_t>(part) * in.n / parts) + wave;
-  const int i1 = static_cast<int>(static_cast<int64_t>(part + 1) * in.n / parts);
+  const int each = in.n / parts, rest = in.n - each * parts;
+  int i = part * each + min(part, rest);
+  const int i1 = i + each + (part < rest ? 1 : 0);
+  i += wave;
   auto first_row = [&](int i) { return w.t0(in.tile(i)); };
   auto own_row = [&](int n) { return first_row(min(i + n * kWinWaves, i1 - 1)); };  // the wave's n-th tile from here, or the last
   int2 blk{};  // of the next tile to be requested
@@ -594,6 +601,7 @@ kv4_kernel(const WindowArgs a, const Kv4Cache four) {
     if (i + kWinWaves < i1) request(own_row(1), blocks_of(own_row(1)), k1, v1);
     blk = blocks_of(own_row(2));
   }
+  q.split();
   // The outer tiles, a few at the ends of what is seen, go round the parts
 #pragma unroll 1
   for (int e = part + wave * parts; e < in.outer; e += kWinWaves * parts) {
@@ -658,16 +666,20 @@ kv4_kernel(const WindowArgs a, const Kv4Cache four) {
     ws.l[wave][n16] = l;
   }
   __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
+  // (the 16-byte pieces of a row change places by its column, so that columns do not meet on
+  // the same banks)
+  auto piece = [](int column, int c) { return 4 * (c ^ (column & 7)); };
   float* mine = reinterpret_cast<float*>(col < COLUMNS / 2 ? k0 : v0) + col % (COLUMNS / 2) * D;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
+    const int dim = (D / 16) * (4 * a4 + r);
     if constexpr (FOLD) {
 #pragma unroll
-      for (int i = 0; i < out.N; ++i) mine[(D / 16) * (4 * a4 + r) + 2 * i + (n16 >> 3)] = out.acc[i][r];
+      for (int i = 0; i < out.N; ++i) mine[piece(col, (dim + 2 * i) / 4) + 2 * (i & 1) + (n16 >> 3)] = out.acc[i][r];
     } else {
 #pragma unroll
       for (int e = 0; e < out.N; e += 4)
-        *reinterpret_cast<float4*>(mine + (D / 16) * (4 * a4 + r) + e) =
+        *reinterpret_cast<float4*>(mine + piece(col, (dim + e) / 4)) =
             make_float4(out.acc[e][r], out.acc[e + 1][r], out.acc[e + 2][r], out.acc[e + 3][r]);
     }
   }
@@ -685,7 +697,8 @@ kv4_kernel(const WindowArgs a, const Kv4Cache four) {
 #pragma unroll
     for (int v = 0; v < kWinWaves; ++v) {
       const float f = weight_of(a, ws.m[v][h], M);
-      const float4 x = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(h < COLUMNS / 2 ? lds_k0 + v * FIRST : lds_v0 + v * (FIRST + SCALES)) + h % (COLUMNS / 2) * D)[c];
+      const unsigned char* place = h < COLUMNS / 2 ? lds_k0 + v * FIRST : lds_v0 + v * (FIRST + SCALES);
+      const float4 x = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(place) + h % (COLUMNS / 2) * D + piece(h, c));
       den = fmaf(f, ws.l[v][h], den);
       o.x = fmaf(f, x.x, o.x);
       o.y = fmaf(f, x.y, o.y);
@@ -744,9 +757,10 @@ WindowPlan make_kv4_plan(const vp_shape& s, const vp_window& w) {
   const bool one_each = tiles <= 28 || brief || (cut && pairs >= 192) || pairs * tiles > 0x3fffffff;
   // Otherwise two work-groups per CU (three or four, where registers allow them: 64 x 32k
   // 190 and 190, 16 x 12k ragged 21.3 and 22.3 to 24.2), twice as many as pairs where those are
-  // more, a tile per wave at least; and no more than 32 for a walk, whose pieces the second
-  // launch joins (1 sequence of 8k: 11.0 and, 64 each, 12.1; of 32k 14.9 and, 128 each, 19.2)
-  const int64_t most = std::min<int64_t>(std::max<int64_t>(512, 2 * pairs), 32 * pairs);
+  // more, a tile per wave at least; and no more than 32 for a walk, or one per 16 tiles, as the second
+  // launch joins the pieces (1 sequence of 8k: 32 each 11.0, 64 each 12.1; of 32k: 64 each 14.6, 128
+  // each 19.2)
+  const int64_t most = std::min<int64_t>(std::max<int64_t>(512, 2 * pairs), pairs * std::max<int64_t>(32, tiles / 16));
   p.groups = one_each ? 0 : static_cast<int>(std::min(most, pairs * ((tiles + kWinWaves - 1) / kWinWaves)));
   carve_window_plan(p, s, false);
   return p;
