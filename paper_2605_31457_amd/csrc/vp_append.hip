@@ -178,6 +178,7 @@ __global__ __launch_bounds__(64 * kAppendWaves) void append_kernel(const AppendA
   constexpr int LANES = D / 8;      // lanes of a row
   constexpr int ROWS = 64 / LANES;  // rows of a wave
   constexpr int BATCH = 3;  // rows of a lane whose loads are in flight together
+  read_early(a.k, a.four.vc, a.block_table, a.cos_sin);
   const int lane = threadIdx.x & 63;
   const int64_t id = static_cast<int64_t>(blockIdx.x) * kAppendWaves + __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   if (id >= static_cast<int64_t>(a.n_tokens) * a.waves) return;

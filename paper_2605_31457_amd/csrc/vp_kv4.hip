@@ -50,6 +50,7 @@ __global__ __launch_bounds__(kReadThreads) void read_kernel(const ReadArgs a) {
   constexpr int LANES = D / 8;
   constexpr int ROWS = kReadThreads / LANES;
   constexpr int BATCH = 4;
+  read_early(a.four.kc, a.K, a.block_table, a.first);
   const int g = blockIdx.y, b = blockIdx.z >> 1;
   const bool value = blockIdx.z & 1;
   const int octet = threadIdx.x % LANES;
@@ -447,6 +448,7 @@ kv4_kernel(const WindowArgs a, const Kv4Cache four) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds_k2[kWinWaves * Q::BYTES];
   __shared__ __attribute__((aligned(1024))) unsigned char lds_v2[kWinWaves * (Q::BYTES + SCALES)];
   __shared__ WinStats ws;
+  read_early(a.q, a.seq_len, a.zscale, four.vs);
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const int lane = threadIdx.x & 63;
   const int n16 = lane & 15;

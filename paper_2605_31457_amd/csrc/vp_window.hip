@@ -505,6 +505,7 @@ template <int DT, int D>
 __global__ __launch_bounds__(kFinishThreads) void finish_kernel(const WindowArgs a, int heads) {
   constexpr int COLS = D / 4;
   constexpr int R = kFinishThreads / COLS;
+  read_early(a.out, a.seq_len, a.stats, heads);
   const int g = blockIdx.y, b = blockIdx.z;
   const int tid = threadIdx.x;
   const size_t pair = static_cast<size_t>(b) * a.Hkv + g;
