@@ -100,23 +100,31 @@ __device__ __forceinline__ int sequence_of(const int32_t* off, int B, int token,
   return lo + __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < n && off[lo + 1 + lane] <= token));
 }
 
-// cosines and sines of a lane's elements: those of its 8 pairs, or (neighbours paired) 4 pairs
+// cosines and sines of a lane's elements: those of its 8 pairs, or (neighbours paired) 4 pairs,
+// in two parts of 4 pairs, which have one axis each
 struct Turn {
   float c[8], s[8];
 };
 
-__device__ __forceinline__ void load_turn(const AppendArgs& a, Turn& t, int octet, int token, int row) {
+__device__ __forceinline__ int pair_of(const AppendArgs& a, int octet, int part) {
+  const int half = a.rot >> 1;
+  if (a.interleaved) return 4 * octet;  // (both parts the same)
+  return (8 * octet >= half ? 8 * octet - half : 8 * octet) + 4 * part;
+}
+
+__device__ __forceinline__ int position_of(const AppendArgs& a, int octet, int part, int token) {
+  const int pair = pair_of(a, octet, part);
+  int axis = 0;
+  for (int x = 0; x + 1 < a.axes; ++x) axis += pair >= a.section_end[x];
+  return a.pos[static_cast<int64_t>(axis) * a.n_tokens + token];
+}
+
+__device__ __forceinline__ void load_turn(const AppendArgs& a, Turn& t, int octet, const int (&pos)[2]) {
   const int half = a.rot >> 1;
 #pragma unroll
   for (int part = 0; part < 2; ++part) {
-    int pair;
-    if (a.interleaved) pair = 4 * octet;  // (both parts the same)
-    else pair = (8 * octet >= half ? 8 * octet - half : 8 * octet) + 4 * part;
-    int axis = 0;
-    for (int x = 0; x + 1 < a.axes; ++x) axis += pair >= a.section_end[x];
-    int p = a.pos ? a.pos[static_cast<int64_t>(axis) * a.n_tokens + token] : row;
-    p = min(max(p, 0), a.n_pos - 1);
-    const float* src = a.cos_sin + static_cast<int64_t>(p) * a.rot + pair;
+    const int p = min(max(pos[part], 0), a.n_pos - 1);
+    const float* src = a.cos_sin + static_cast<int64_t>(p) * a.rot + pair_of(a, octet, part);
     const float4 c = *reinterpret_cast<const float4*>(src);
     const float4 s = *reinterpret_cast<const float4*>(src + half);
     t.c[4 * part + 0] = c.x;
@@ -185,10 +193,44 @@ __global__ __launch_bounds__(64 * kAppendWaves) void append_kernel(const AppendA
   const int token = static_cast<int>(id / a.waves);
   const int first = static_cast<int>(id - static_cast<int64_t>(token) * a.waves) * ROWS;
 
+  const int octet = lane % LANES;
+  const bool turns = 8 * octet < a.rot;
+  const int half = a.rot >> 1;
+  const bool upper = 8 * octet >= half;
+  const int partner = !turns || a.interleaved ? octet : upper ? octet - half / 8 : octet + half / 8;
+  const int Hq = a.q ? a.Hq : 0;
+  const int rows = Hq + 2 * a.Hkv;
+  const int step = a.waves * ROWS;
+  const char* const qs = static_cast<const char*>(a.q) + token * a.qs;
+  const char* const ks = static_cast<const char*>(a.k) + token * a.ks;
+  const char* const vs = static_cast<const char*>(a.v) + token * a.vs;
+  Octet<DT> x[BATCH], y[BATCH];
+  auto load = [&](int r0) {
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) {
+      const int r = min(r0 + j * step, rows - 1);
+      const bool key = r < Hq + a.Hkv;
+      const char* src = r < Hq ? qs + r * (D * ESZ) : key ? ks + (r - Hq) * (D * ESZ) : vs + (r - Hq - a.Hkv) * (D * ESZ);
+      x[j].load(src + octet * (8 * ESZ));
+      y[j].load(src + (key ? partner : octet) * (8 * ESZ));
+    }
+  };
+  // Requested together, in the order of their use: the offsets (up to 64 sequences: one of
+  // each lane), the positions, the first rows
+  const bool few = a.B <= 64;
+  int end = 0x7fffffff;
+  if (a.new_off && few && lane < a.B) end = a.new_off[1 + lane];
+  int pos[2] = {0, 0};
+  if (turns && a.pos) {
+    pos[0] = position_of(a, octet, 0, token);
+    pos[1] = position_of(a, octet, 1, token);
+  }
+  load(first + lane / LANES);
+
   // the token's sequence and row
   int b, i, n;
   if (a.new_off) {
-    b = sequence_of(a.new_off, a.B, token, lane);
+    b = few ? __builtin_popcountll(__builtin_amdgcn_ballot_w64(end <= token)) : sequence_of(a.new_off, a.B, token, lane);
     if (b >= a.B) return;  // (behind the last sequence)
     const int64_t o = a.new_off[b];
     const int64_t len = a.new_off[b + 1] - o;
@@ -208,31 +250,11 @@ __global__ __launch_bounds__(64 * kAppendWaves) void append_kernel(const AppendA
     at = a.block_table[static_cast<int64_t>(b) * a.nblk + (row >> a.bs_log2)];
     in = row & ((1 << a.bs_log2) - 1);
   }
-
-  const int octet = lane % LANES;
-  const bool turns = 8 * octet < a.rot;
-  const int half = a.rot >> 1;
-  const bool upper = 8 * octet >= half;
-  const int partner = !turns || a.interleaved ? octet : upper ? octet - half / 8 : octet + half / 8;
+  if (!a.pos) pos[0] = pos[1] = row;
   Turn turn{};
-  if (turns) load_turn(a, turn, octet, token, row);
+  if (turns) load_turn(a, turn, octet, pos);
 
-  const int Hq = a.q ? a.Hq : 0;
-  const int rows = Hq + 2 * a.Hkv;
-  const int step = a.waves * ROWS;
-  const char* const qs = static_cast<const char*>(a.q) + token * a.qs;
-  const char* const ks = static_cast<const char*>(a.k) + token * a.ks;
-  const char* const vs = static_cast<const char*>(a.v) + token * a.vs;
-  for (int r0 = first + lane / LANES; r0 - lane / LANES < rows; r0 += BATCH * step) {
-    Octet<DT> x[BATCH], y[BATCH];
-#pragma unroll
-    for (int j = 0; j < BATCH; ++j) {
-      const int r = min(r0 + j * step, rows - 1);
-      const bool key = r < Hq + a.Hkv;
-      const char* src = r < Hq ? qs + r * (D * ESZ) : key ? ks + (r - Hq) * (D * ESZ) : vs + (r - Hq - a.Hkv) * (D * ESZ);
-      x[j].load(src + octet * (8 * ESZ));
-      y[j].load(src + (key ? partner : octet) * (8 * ESZ));
-    }
+  for (int r0 = first + lane / LANES;;) {
 #pragma unroll
     for (int j = 0; j < BATCH; ++j) {
       const int r = r0 + j * step;
@@ -270,6 +292,9 @@ __global__ __launch_bounds__(64 * kAppendWaves) void append_kernel(const AppendA
         x[j].store(dst + octet * (8 * ESZ));
       }
     }
+    r0 += BATCH * step;
+    if (r0 - lane / LANES >= rows) break;
+    load(r0);
   }
 }
 
