@@ -377,6 +377,7 @@ WindowArgs window_args(const vp_shape* shape, const vp_layout* layout, const vp_
   a.Hkv = shape->n_kv_heads;
   a.G = shape->n_q_heads / shape->n_kv_heads;
   a.T = queries(*shape);
+  a.over_g = 65536u / a.G + 1;
   a.max_seq_len = shape->max_seq_len;
   a.window = std::min(window->window, 2 * kMaxTokens);  // (further back than any row)
   a.n_sink = window->n_sink;

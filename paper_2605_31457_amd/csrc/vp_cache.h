@@ -35,6 +35,7 @@ struct WindowArgs {
   const int32_t* seq_len;
   int B, Hq, Hkv, G, T, max_seq_len;
   int window, n_sink;
+  uint32_t over_g;             // r / G = r * over_g >> 16 for query rows r < 16
   float zscale;                // sm_scale * log2(e)
   float raise;                 // a running maximum is raised when a product exceeds it by more
   int tiles, groups, gp;

@@ -458,7 +458,7 @@ kv4_kernel(const WindowArgs a, const Kv4Cache four) {
   const int col = n16 & (COLUMNS - 1);  // this lane's query row
   const int TG = a.T * a.G;
   const bool hv = col < TG;
-  const int tq = hv ? col / a.G : 0;
+  const int tq = hv ? query_of(a, col) : 0;
 
   const bool dealt = a.groups > 0;
   int g = blockIdx.y, b = blockIdx.z, part = 0, parts = 1, L;

@@ -51,8 +51,10 @@ __device__ __forceinline__ void store_out(void* out, size_t row, int D, int col4
 }
 
 // row of out [B][T][Hq] for query row r (query t = r / G, head g*G + r % G)
+__device__ __forceinline__ int query_of(const WindowArgs& a, int r) { return static_cast<int>(r * a.over_g >> 16); }
 __device__ __forceinline__ size_t out_row(const WindowArgs& a, int b, int g, int r) {
-  return (static_cast<size_t>(b) * a.T + r / a.G) * a.Hq + g * a.G + r % a.G;
+  const int t = query_of(a, r);
+  return (static_cast<size_t>(b) * a.T + t) * a.Hq + g * a.G + (r - t * a.G);
 }
 
 __device__ __forceinline__ WindowWalk walk_of(const WindowArgs& a, int b) {

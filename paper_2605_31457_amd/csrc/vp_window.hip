@@ -210,7 +210,7 @@ window_kernel(const WindowArgs a) {
   const unsigned char* vb = lds_v + wave * Q::V_BYTES;
   float* stage = reinterpret_cast<float*>(lds_stage + wave * Q::STAGE_BYTES);
   const bool hv = n16 < TG;
-  const int tq = hv ? n16 / a.G : 0;
+  const int tq = hv ? query_of(a, n16) : 0;
 
   const bool dealt = a.groups > 0;
   int g = blockIdx.y, b = blockIdx.z, part = 0, parts = 1, L;
