@@ -255,7 +255,9 @@ class DeviceStep:
         if new_off is not None and (new_off.dtype != torch.int32 or new_off.numel() != self.w.B + 1
                                     or not new_off.is_contiguous() or new_off.device != self.K.device):
             raise ValueError(f"append: new_off must be int32 [{self.w.B + 1}] on {self.K.device}")
-        pos = getattr(rope, "tensors", (None, None))[1]
+        cos_sin, pos = getattr(rope, "tensors", (None, None))
+        if cos_sin is not None and cos_sin.device != self.K.device:
+            raise ValueError(f"append: the rotation's cos_sin is on {cos_sin.device}, not {self.K.device}")
         if pos is not None and pos.shape[-1] != n:
             raise ValueError(f"append: positions of {pos.shape[-1]} tokens for {n}")
         if q is not None and q_out is None:

@@ -1,0 +1,17 @@
+"""DeviceStep.append before anything is enqueued (no GPU): what it refuses and what it passes on."""
+import pytest
+import torch
+
+from paper_2605_31457_amd import step as S
+from _parity import small_workload
+
+
+def _step(Hkv=1, device="cpu"):
+    return S.DeviceStep(small_workload(5, 2, 4, Hkv, 64, [50, 20], [[], []]), device=device, max_vis=1)
+
+
+def test_rope_on_another_device():
+    ds = _step(device="meta")
+    k = torch.zeros(2, 1, 64, dtype=torch.bfloat16, device="meta")
+    with pytest.raises(ValueError, match="cos_sin"):
+        ds.append(k, k, rope=S.make_rope(torch.zeros(64, 64)))
