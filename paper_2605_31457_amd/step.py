@@ -271,7 +271,9 @@ class DeviceStep:
                               v_stride=step(v, self.w.Hkv), new_off=None if new_off is None else new_off.data_ptr(),
                               n_tokens=n)
         if four:
-            vp.vp_append_kv4(self.shape, self.layout, rope, tokens, q_out, self._kv4("append"), stream)
+            cache = self._kv4("append")
+            vp._on_current_device("append", k)  # (structs and, without queries, no tensor reach the binding)
+            vp.vp_append_kv4(self.shape, self.layout, rope, tokens, q_out, cache, stream)
         else:
             vp.vp_append_kv(self.shape, self.layout, rope, tokens, q_out, self.K, self.V, stream)
         return q_out

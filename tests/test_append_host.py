@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from paper_2605_31457_amd import step as S
+from paper_2605_31457_amd import vp
 from _parity import small_workload
 
 
@@ -15,3 +16,14 @@ def test_rope_on_another_device():
     k = torch.zeros(2, 1, 64, dtype=torch.bfloat16, device="meta")
     with pytest.raises(ValueError, match="cos_sin"):
         ds.append(k, k, rope=S.make_rope(torch.zeros(64, 64)))
+
+
+@pytest.mark.parametrize("four", [False, True])
+def test_another_current_device(four, monkeypatch):
+    ds = _step()
+    ds.make_kv4()
+    monkeypatch.setattr(vp, "_current_device", lambda: 0)  # (the buffers are on none)
+    monkeypatch.setattr(vp, "_stream", lambda s: 0)
+    k = torch.zeros(2, 1, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="current device"):
+        ds.append(k, k, four=four)
