@@ -250,7 +250,7 @@ class DeviceStep:
             if tuple(x.shape) != (n, heads, d) or x.dtype != self.q.dtype or x.device != self.K.device:
                 raise ValueError(f"append: {name} is {x.dtype} {tuple(x.shape)} on {x.device}, not {self.q.dtype} "
                                  f"{(n, heads, d)} on {self.K.device}")
-            if n and (x.stride(2) != 1 or x.stride(1) != d):
+            if n and (x.stride(2) != 1 or (heads > 1 and x.stride(1) != d)):
                 raise ValueError(f"append: a token's heads in {name} must lie next to each other")
         if new_off is not None and (new_off.dtype != torch.int32 or new_off.numel() != self.w.B + 1
                                     or not new_off.is_contiguous() or new_off.device != self.K.device):

@@ -27,3 +27,18 @@ def test_another_current_device(four, monkeypatch):
     k = torch.zeros(2, 1, 64, dtype=torch.bfloat16)
     with pytest.raises(ValueError, match="current device"):
         ds.append(k, k, four=four)
+
+
+def test_one_head_of_any_stride(monkeypatch):
+    """With one KV head the stride between heads means nothing."""
+    ds = _step()
+    seen = []
+    monkeypatch.setattr(vp, "vp_append_kv", lambda shape, layout, rope, tokens, *a: seen.append((tokens.k_stride, tokens.v_stride)))
+    x = torch.zeros(2, 256, dtype=torch.bfloat16)
+    k, v = x[:, 64:128].as_strided((2, 1, 64), (256, 8, 1), 64), torch.zeros(1, 2, 64, dtype=torch.bfloat16).transpose(0, 1)
+    ds.append(k, v)
+    assert seen == [(256, 64)]
+    with pytest.raises(ValueError, match="next to each other"):
+        _step(Hkv=2).append(torch.zeros(2, 64, 2, dtype=torch.bfloat16).transpose(1, 2), torch.zeros(2, 2, 64, dtype=torch.bfloat16))
+    with pytest.raises(ValueError, match="next to each other"):
+        ds.append(torch.zeros(2, 1, 128, dtype=torch.bfloat16)[..., ::2], v)
