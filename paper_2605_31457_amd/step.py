@@ -222,7 +222,9 @@ class DeviceStep:
     # appending, and a cache of 4 bits ---------------------------------------
     def make_kv4(self):
         """A 4-bit cache for these sequences, of the same blocks where caches are paged: codes
-        and scales of K and V (``kv4_codes``, ``kv4_scales``), what lies in them unset."""
+        and scales of K and V (``kv4_codes``, ``kv4_scales``), what lies in them unset. Called
+        again it makes another: graphs captured before hold the addresses of the first,
+        which the caller keeps alive for them."""
         n, rows = self.K.shape[0], -(-self.K.shape[2] // 16) * 16
         u8 = lambda width: [torch.empty(n, self.w.Hkv, rows, width, dtype=torch.uint8, device=self.device) for _ in range(2)]
         self.kv4_codes, self.kv4_scales = u8(self.w.d // 2), u8(self.w.d // 32)
