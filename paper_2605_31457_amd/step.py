@@ -222,7 +222,9 @@ class DeviceStep:
     # appending, and a cache of 4 bits ---------------------------------------
     def make_kv4(self):
         """A 4-bit cache for these sequences, of the same blocks where caches are paged: codes
-        and scales of K and V (``kv4_codes``, ``kv4_scales``), what lies in them unset. Called
+        and scales of K and V (``kv4_codes``, ``kv4_scales``), what lies in them unset: every
+        row below ``seq_len``, a prompt's too, has to be appended with ``four=True`` before
+        ``kv4_decode_attn`` or ``kv4_read`` (from ``first`` on) read it. Called
         again it makes another: graphs captured before hold the addresses of the first,
         which the caller keeps alive for them."""
         n, rows = self.K.shape[0], -(-self.K.shape[2] // 16) * 16
@@ -290,7 +292,8 @@ class DeviceStep:
         vp.vp_kv4_decode_attn(self.shape, self.layout, opt, self.q, cache, self.out, ws, nbytes, stream)
 
     def kv4_read(self, first=None, stream=None):
-        """vp_kv4_read: the 4-bit cache's rows from first[b] on (int32 [B]; None: all) into K and V."""
+        """vp_kv4_read: the 4-bit cache's rows from first[b] on (int32 [B]; None: all) into K and V,
+        whose rows they replace."""
         if first is not None and (first.dtype != torch.int32 or first.numel() != self.w.B or not first.is_contiguous()):
             raise ValueError(f"kv4_read: first must be int32 [{self.w.B}]")
         vp.vp_kv4_read(self.shape, self.layout, self._kv4("kv4_read"), first, self.K, self.V, stream)
