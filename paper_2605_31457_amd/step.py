@@ -246,7 +246,8 @@ class DeviceStep:
         [n, Hkv, d] and, if given, q [n, Hq, d] (slices of one product's columns will do) to the last
         rows of their sequences, whose ``seq_len`` counts them already. new_off int32 [B+1]: how
         many each sequence has (None: the step's queries each, n = B * T). Rotated queries go to
-        q_out (None: ``q``, the step's queries; n = B * T then). Returns q_out."""
+        q_out; None is ``q``, the step's queries, where new_off is None too. n = 0 (with new_off)
+        appends nothing. Returns q_out."""
         n, d = k.shape[0], self.w.d
         for name, x, heads in (("k", k, self.w.Hkv), ("v", v, self.w.Hkv), ("q", q, self.w.Hq)):
             if x is None:
@@ -264,7 +265,10 @@ class DeviceStep:
             raise ValueError(f"append: the rotation's cos_sin is on {cos_sin.device}, not {self.K.device}")
         if pos is not None and pos.shape[-1] != n:
             raise ValueError(f"append: positions of {pos.shape[-1]} tokens for {n}")
-        if q is not None and q_out is None:
+        if q is not None and q_out is None and n:
+            if new_off is not None:  # (the counts are on the device)
+                raise ValueError("append: queries of as many tokens as new_off says need a q_out; the step's own queries, "
+                                 "q, are one after another for T tokens of every sequence")
             q_out = self.q
         if q_out is not None and (q is None or q_out.numel() != n * self.w.Hq * d or q_out.dtype != self.q.dtype
                                   or not q_out.is_contiguous()):
