@@ -373,8 +373,8 @@ vp_status vp_window_workspace_size(const vp_shape* shape, const vp_window* windo
  * call on the same inputs gives the same bits.
  *
  * layout: seq_len (and block_table with paged caches); the segments are not
- * read. shape.max_vis, max_segs, k_cap and scope have no effect. The workspace
- * must not be shared by concurrent calls.
+ * read. shape.max_vis, max_segs, k_cap and scope are not looked at (zeros will
+ * do). The workspace must not be shared by concurrent calls.
  * VP_ERR_RANGE: window < 0, n_sink < 0, sm_scale not finite.
  */
 vp_status vp_window_decode_attn(const vp_shape* shape, const vp_layout* layout, const vp_window* window,
@@ -429,7 +429,8 @@ vp_status vp_evict_workspace_size(const vp_shape* shape, const vp_evict_params* 
  * Rows from new_len on, of K, V and attn_sum_out, are left as they are. The
  * visual segments are read only for vis_seg_out. A block that two sequences
  * share (or a sequence twice) must not be evicted from: block ids are trusted.
- * shape.n_queries, max_vis, max_segs and k_cap have no effect on the rows kept.
+ * shape.n_queries, max_vis, max_segs and k_cap have no effect on the rows kept
+ * (they have to be those of a valid step).
  * K and V must be different caches whose rows do not overlap (VP_ERR_SHAPE for
  * strides that make them), and the workspace must not be shared by concurrent
  * calls.
@@ -447,7 +448,7 @@ vp_status vp_evict(const vp_shape* shape, const vp_layout* layout, const vp_evic
  * vp_kv4_decode_attn attends and from which vp_kv4_read brings rows back.
  * layout: seq_len counts the new tokens already, as it does for the step's attention
  * (and block_table with paged caches); the segments are not read and may be NULL.
- * shape.max_vis, max_segs, k_cap and scope have no effect.
+ * shape.max_vis, max_segs, k_cap and scope are not looked at (zeros will do).
  */
 
 /* Rotation of queries and keys by position. Of every head the first rot_dim elements
@@ -522,7 +523,7 @@ vp_status vp_append_kv(const vp_shape* shape, const vp_layout* layout, const vp_
  * even code, at most 6: an element is off by half a step of its code, a quarter of it at most where
  * it is above the scale, and 0.25 of the scale below. Codes are those of the 64-bit values. 32 elements among which
  * is an infinity or NaN become NaN, all of them (scale byte 255). shape's K and V strides
- * have no effect. The rows of a cache must not overlap (VP_ERR_SHAPE).
+ * are not looked at. The rows of a cache must not overlap (VP_ERR_SHAPE).
  * VP_ERR_UNSUPPORTED: block_size below 16.
  */
 vp_status vp_append_kv4(const vp_shape* shape, const vp_layout* layout, const vp_rope* rope, const vp_tokens* tokens,
@@ -545,7 +546,7 @@ vp_status vp_kv4_workspace_size(const vp_shape* shape, const vp_window* window, 
  * vp_kv4_decode_attn -- vp_window_decode_attn (without sums) over a 4-bit cache: the same
  * positions seen, [B, T, Hq, d] in and out, zeros for a query that sees nothing or whose
  * logits are all -inf, no influence of rows that a query does not see. Products and sums are formed in 32 bits
- * from the values that the codes stand for. Strides of K and V in shape have no effect.
+ * from the values that the codes stand for. Strides of K and V in shape are not looked at.
  * The workspace must not be shared by concurrent calls.
  */
 vp_status vp_kv4_decode_attn(const vp_shape* shape, const vp_layout* layout, const vp_window* window, const void* q,

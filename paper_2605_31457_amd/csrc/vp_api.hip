@@ -71,7 +71,8 @@ constexpr int kMaxNewTokens = 1 << 24;  // tokens that a call appends (a wave or
 constexpr int kMaxTokens = 1 << 28;  // bound on max_seq_len, max_vis and k_cap (32-bit index arithmetic)
 
 
-vp_status check_shape(const vp_shape* s) {
+// The fields of vp_shape that every call uses
+vp_status check_sizes(const vp_shape* s) {
   if (!s) return fail(VP_ERR_NULL, "shape is NULL");
   if (s->dtype != VP_F32 && s->dtype != VP_BF16) return fail(VP_ERR_DTYPE, "dtype %d", s->dtype);
   if (s->batch < 1 || s->batch > kMaxBatch) return fail(VP_ERR_SHAPE, "batch %d outside [1, %d]", s->batch, kMaxBatch);
@@ -83,29 +84,48 @@ vp_status check_shape(const vp_shape* s) {
   if (s->n_q_heads > kMaxHq) return fail(VP_ERR_UNSUPPORTED, "n_q_heads %d > %d", s->n_q_heads, kMaxHq);
   if (s->head_dim != 64 && s->head_dim != 128) return fail(VP_ERR_UNSUPPORTED, "head_dim %d (64 or 128)", s->head_dim);
   if (s->max_seq_len < 1) return fail(VP_ERR_SHAPE, "max_seq_len %d < 1", s->max_seq_len);
-  if (s->max_vis < 1) return fail(VP_ERR_SHAPE, "max_vis %d < 1", s->max_vis);
-  if (s->max_seq_len > kMaxTokens || s->max_vis > kMaxTokens || s->k_cap > kMaxTokens)
-    return fail(VP_ERR_UNSUPPORTED, "max_seq_len, max_vis and k_cap must not exceed %d", kMaxTokens);
-  if (s->max_segs < 0 || s->max_segs > 256) return fail(VP_ERR_UNSUPPORTED, "max_segs %d outside [0, 256]", s->max_segs);
-  if (s->k_cap < 1) return fail(VP_ERR_SHAPE, "k_cap %d < 1", s->k_cap);
+  if (s->max_seq_len > kMaxTokens) return fail(VP_ERR_UNSUPPORTED, "max_seq_len %d > %d", s->max_seq_len, kMaxTokens);
   if (s->block_size < 0 || s->block_size > 65536 || (s->block_size & (s->block_size - 1)) != 0)
     return fail(VP_ERR_SHAPE, "block_size %d: 0 (contiguous) or a power of two <= 65536", s->block_size);
-  if (s->scope != VP_SCOPE_SEQUENCE && s->scope != VP_SCOPE_KV_GROUP)
-    return fail(VP_ERR_RANGE, "scope %d: VP_SCOPE_SEQUENCE or VP_SCOPE_KV_GROUP", s->scope);
   if (s->n_queries < 0) return fail(VP_ERR_RANGE, "n_queries %d < 0", s->n_queries);
   if (static_cast<int64_t>(queries(*s)) * (s->n_q_heads / s->n_kv_heads) > kMaxGroup)
     return fail(VP_ERR_UNSUPPORTED, "n_queries %d x query group %d > %d rows per KV head", queries(*s),
                 s->n_q_heads / s->n_kv_heads, kMaxGroup);
-  if (static_cast<int64_t>(s->batch) * rows_per_seq(*s) > kMaxBatch)
-    return fail(VP_ERR_UNSUPPORTED, "batch x queries x selection rows %lld > %d",
-                static_cast<long long>(s->batch) * rows_per_seq(*s), kMaxBatch);
-  const int esz = s->dtype == VP_BF16 ? 2 : 4;
-  const int64_t align_elems = 16 / esz;
+  if (static_cast<int64_t>(s->batch) * queries(*s) > kMaxBatch)
+    return fail(VP_ERR_UNSUPPORTED, "batch x queries %lld > %d", static_cast<long long>(s->batch) * queries(*s), kMaxBatch);
+  return VP_OK;
+}
+
+// Strides of 16- and 32-bit caches
+vp_status check_strides(const vp_shape* s) {
+  const int64_t align_elems = s->dtype == VP_BF16 ? 8 : 4;
   if (s->kv_stride_s < s->head_dim) return fail(VP_ERR_SHAPE, "kv_stride_s %lld < head_dim", (long long)s->kv_stride_s);
   if (s->kv_stride_b < 0 || s->kv_stride_h < 0) return fail(VP_ERR_SHAPE, "negative KV stride");
   if (s->kv_stride_s % align_elems || s->kv_stride_h % align_elems || s->kv_stride_b % align_elems)
     return fail(VP_ERR_SHAPE, "KV strides must be multiples of %lld elements (16-byte rows)", (long long)align_elems);
   return VP_OK;
+}
+
+// The calls on such caches to which visual tokens and their selection do not matter
+vp_status check_caches(const vp_shape* s) {
+  if (vp_status e = check_sizes(s)) return e;
+  return check_strides(s);
+}
+
+// All fields
+vp_status check_shape(const vp_shape* s) {
+  if (vp_status e = check_sizes(s)) return e;
+  if (s->max_vis < 1) return fail(VP_ERR_SHAPE, "max_vis %d < 1", s->max_vis);
+  if (s->max_vis > kMaxTokens || s->k_cap > kMaxTokens)
+    return fail(VP_ERR_UNSUPPORTED, "max_vis and k_cap must not exceed %d", kMaxTokens);
+  if (s->max_segs < 0 || s->max_segs > 256) return fail(VP_ERR_UNSUPPORTED, "max_segs %d outside [0, 256]", s->max_segs);
+  if (s->k_cap < 1) return fail(VP_ERR_SHAPE, "k_cap %d < 1", s->k_cap);
+  if (s->scope != VP_SCOPE_SEQUENCE && s->scope != VP_SCOPE_KV_GROUP)
+    return fail(VP_ERR_RANGE, "scope %d: VP_SCOPE_SEQUENCE or VP_SCOPE_KV_GROUP", s->scope);
+  if (static_cast<int64_t>(s->batch) * rows_per_seq(*s) > kMaxBatch)
+    return fail(VP_ERR_UNSUPPORTED, "batch x queries x selection rows %lld > %d",
+                static_cast<long long>(s->batch) * rows_per_seq(*s), kMaxBatch);
+  return check_strides(s);
 }
 
 vp_status check_params(const vp_params* p) {
@@ -885,7 +905,7 @@ vp_status vp_decode_step_static(const vp_shape* shape, const vp_layout* layout, 
 
 vp_status vp_window_workspace_size(const vp_shape* shape, const vp_window* window, int32_t with_sums, size_t* bytes) {
   g_last_error.clear();
-  if (vp_status e = check_shape(shape)) return e;
+  if (vp_status e = check_caches(shape)) return e;
   if (vp_status e = check_window(window)) return e;
   if (with_sums != 0 && with_sums != 1) return fail(VP_ERR_RANGE, "with_sums must be 0 or 1");
   if (!bytes) return fail(VP_ERR_NULL, "bytes is NULL");
@@ -897,7 +917,7 @@ vp_status vp_window_decode_attn(const vp_shape* shape, const vp_layout* layout, 
                                 const void* K, const void* V, float* attn_sum, void* out, void* workspace,
                                 size_t workspace_bytes, void* stream) {
   g_last_error.clear();
-  if (vp_status e = check_shape(shape)) return e;
+  if (vp_status e = check_caches(shape)) return e;
   if (vp_status e = check_rows(shape, layout)) return e;
   if (vp_status e = check_window(window)) return e;
   if (!q || !K || !V || !out) return fail(VP_ERR_NULL, "q, K, V, out required");
@@ -985,7 +1005,7 @@ vp_status vp_evict(const vp_shape* shape, const vp_layout* layout, const vp_evic
 vp_status vp_append_kv(const vp_shape* shape, const vp_layout* layout, const vp_rope* rope, const vp_tokens* tokens,
                        void* q_out, void* K, void* V, void* stream) {
   g_last_error.clear();
-  if (vp_status e = check_shape(shape)) return e;
+  if (vp_status e = check_caches(shape)) return e;
   if (vp_status e = check_rows(shape, layout)) return e;
   if (vp_status e = check_rope(shape, rope)) return e;
   if (vp_status e = check_tokens(shape, tokens, q_out)) return e;
@@ -1008,7 +1028,7 @@ vp_status vp_append_kv(const vp_shape* shape, const vp_layout* layout, const vp_
 vp_status vp_append_kv4(const vp_shape* shape, const vp_layout* layout, const vp_rope* rope, const vp_tokens* tokens,
                         void* q_out, const vp_kv4* cache, void* stream) {
   g_last_error.clear();
-  if (vp_status e = check_shape(shape)) return e;
+  if (vp_status e = check_sizes(shape)) return e;
   if (vp_status e = check_rows(shape, layout)) return e;
   if (vp_status e = check_rope(shape, rope)) return e;
   if (vp_status e = check_tokens(shape, tokens, q_out)) return e;
@@ -1023,7 +1043,7 @@ vp_status vp_append_kv4(const vp_shape* shape, const vp_layout* layout, const vp
 vp_status vp_kv4_read(const vp_shape* shape, const vp_layout* layout, const vp_kv4* cache, const int32_t* first, void* K,
                       void* V, void* stream) {
   g_last_error.clear();
-  if (vp_status e = check_shape(shape)) return e;
+  if (vp_status e = check_caches(shape)) return e;
   if (vp_status e = check_rows(shape, layout)) return e;
   if (vp_status e = check_kv4(shape, cache, false)) return e;
   if (!K || !V) return fail(VP_ERR_NULL, "K, V required");
@@ -1056,7 +1076,7 @@ vp_status vp_kv4_read(const vp_shape* shape, const vp_layout* layout, const vp_k
 
 vp_status vp_kv4_workspace_size(const vp_shape* shape, const vp_window* window, size_t* bytes) {
   g_last_error.clear();
-  if (vp_status e = check_shape(shape)) return e;
+  if (vp_status e = check_sizes(shape)) return e;
   if (vp_status e = check_window(window)) return e;
   if (!bytes) return fail(VP_ERR_NULL, "bytes is NULL");
   *bytes = make_kv4_plan(*shape, *window).total;
@@ -1066,7 +1086,7 @@ vp_status vp_kv4_workspace_size(const vp_shape* shape, const vp_window* window, 
 vp_status vp_kv4_decode_attn(const vp_shape* shape, const vp_layout* layout, const vp_window* window, const void* q,
                              const vp_kv4* cache, void* out, void* workspace, size_t workspace_bytes, void* stream) {
   g_last_error.clear();
-  if (vp_status e = check_shape(shape)) return e;
+  if (vp_status e = check_sizes(shape)) return e;
   if (vp_status e = check_rows(shape, layout)) return e;
   if (vp_status e = check_window(window)) return e;
   if (vp_status e = check_kv4(shape, cache, false)) return e;
