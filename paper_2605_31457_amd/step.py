@@ -227,6 +227,8 @@ class DeviceStep:
         ``kv4_decode_attn`` or ``kv4_read`` (from ``first`` on) read it. Called
         again it makes another: graphs captured before hold the addresses of the first,
         which the caller keeps alive for them."""
+        if 0 < self.block_size < 16:
+            raise ValueError(f"make_kv4: blocks of {self.block_size} rows; those of a 4-bit cache hold 16 rows or more")
         n, rows = self.K.shape[0], -(-self.K.shape[2] // 16) * 16
         u8 = lambda width: [torch.empty(n, self.w.Hkv, rows, width, dtype=torch.uint8, device=self.device) for _ in range(2)]
         self.kv4_codes, self.kv4_scales = u8(self.w.d // 2), u8(self.w.d // 32)
