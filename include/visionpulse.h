@@ -359,7 +359,10 @@ vp_status vp_window_workspace_size(const vp_shape* shape, const vp_window* windo
  *
  * A query that sees nothing, or whose logits are all -inf, gives zeros. Rows
  * that a query does not see have no influence on its output, whatever they hold.
- * Rows from seq_len on are not read.
+ * Rows from seq_len on are not read. Products and sums are formed in 32 bits,
+ * those over V before they are normalised, with weights up to 2^16: elements of
+ * V below 2^111 / (rows seen) in magnitude do not overflow them, larger ones may
+ * give infinities and NaN where the mean is finite.
  *
  * attn_sum (optional, else NULL): float [B, Hkv, max_seq_len], the attention
  * weight that every cached row has been given. The call adds, for every row
@@ -546,7 +549,7 @@ vp_status vp_kv4_workspace_size(const vp_shape* shape, const vp_window* window, 
  * vp_kv4_decode_attn -- vp_window_decode_attn (without sums) over a 4-bit cache: the same
  * positions seen, [B, T, Hq, d] in and out, zeros for a query that sees nothing or whose
  * logits are all -inf, no influence of rows that a query does not see. Products and sums are formed in 32 bits
- * from the values that the codes stand for. Strides of K and V in shape are not looked at.
+ * from the values that the codes stand for, with the range that it states. Strides of K and V in shape are not looked at.
  * The workspace must not be shared by concurrent calls.
  */
 vp_status vp_kv4_decode_attn(const vp_shape* shape, const vp_layout* layout, const vp_window* window, const void* q,

@@ -404,8 +404,9 @@ WindowArgs window_args(const vp_shape* shape, const vp_layout* layout, const vp_
   const float sm = window->sm_scale > 0.f ? window->sm_scale : 1.0f / std::sqrt(static_cast<float>(shape->head_dim));
   // log2(e); the largest scales stay finite, as an infinite one makes a NaN of the maximum's weight
   a.zscale = std::min(sm * 1.4426950408889634f, 0x1.fffffep127f);
-  // weights stay below 2^8, and rescaling is rare; small beside the maximum that precedes
-  // the first row (-FLT_MAX), which every product exceeds
+  // weights stay below 2^8 (2^16 at most where m + raise is rounded up, by raise itself at most),
+  // and rescaling is rare; small beside the maximum that precedes the first row (-FLT_MAX),
+  // which every product exceeds
   a.raise = std::min(8.f / a.zscale, 0x1p100f);
   a.tiles = plan.tiles;
   a.groups = plan.groups;
