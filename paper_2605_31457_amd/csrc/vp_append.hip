@@ -8,9 +8,9 @@
 // the sum is rounded once; what is stored is that, rounded once more (to 16 bits through 32:
 // off by at most half a step and 2^-16 of it). So a value does not depend on how the
 // arithmetic is arranged, and 4-bit codes next to a border fall on the right side of it. In 16
-// bits it costs nothing that shows: 10k tokens of 72B-class heads (64/8 of 128) take 82 us, 5.2 TB/s
-// read and written, a large copy's rate. Into 4 bits, with half the bytes written, 12.5k tokens
-// of 28/4 heads take 46 to 53, 4.0 to 4.7 TB/s.
+// bits it costs little: 10k tokens of 72B-class heads (64/8 of 128) take 84 to 86 us in 16 bits, 5.0 TB/s
+// read and written (a large copy: 5.2), 166 in 32. Into 4 bits 12.5k tokens of 28/4 heads take 50
+// to 53, 4.1 to 4.3 TB/s (45 where the same rows come again and lie in the caches).
 //
 // Bound: HBM, every row read and written once; a few tokens: one launch of dependent loads
 // (offsets, length, block id; position, cosines; the rows beside them: 2.6 us for one token). A
@@ -312,9 +312,11 @@ hipError_t launch_dd(const AppendArgs& a, bool four, hipStream_t st) {
 hipError_t launch_append(const AppendArgs& in, bool four, int dtype, int head_dim, hipStream_t st) {
   AppendArgs a = in;
   if (a.n_tokens == 0) return hipSuccess;
-  // A token's rows go to as many waves as fill the GPU, up to one per batch of rows; to a sixth
-  // of that in any case (two rounds of the loop: 10k tokens of 72B-class heads in bf16, 20 batches each: 82 us,
-  // with one wave each 90, with 5 waves that have one row in flight 85). At most 2^26 waves in all.
+  // A token's rows go to as many waves as fill the GPU, up to one per 512 elements (a batch), and
+  // with many tokens to one wave per 6 batches, rounded down (two to four rounds of the loop,
+  // 3 batches each). 10k tokens of 72B-class heads in bf16, 20 batches: 3 waves 85.6 us, 4 (rounded
+  // up) 84.8, 7 101, one 88; in fp32 166, 162, 162, 172. 12.5k of 28/4 heads into 4 bits, 9
+  // batches: one wave 50.4, 2 (rounded up) 55.7, 3 57.6. At most 2^26 waves in all.
   const int batches = ((a.q ? a.Hq : 0) + 2 * a.Hkv + 512 / head_dim - 1) / (512 / head_dim);
   const int64_t fill = std::max<int64_t>(8192 / a.n_tokens, batches / 6);
   a.waves = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({batches, fill, (1 << 26) / a.n_tokens})));

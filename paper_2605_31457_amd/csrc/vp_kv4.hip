@@ -755,7 +755,8 @@ WindowPlan make_kv4_plan(const vp_shape& s, const vp_window& w) {
   //   that 27.8 and 27.8, 256 tiles 55.6 and 57.1, 48.1 and 41.2; 128 sequences, 64 tiles 28.8
   //   and 37.7);
   // * a window cuts the walks of the capacity to half or less, and the pairs nearly fill the
-  //   CUs (as above: equal walks).
+  //   CUs (64 sequences, window 8192 of 32k: 56.4 and 58.1, lengths from 1k on 55.0 and 55.5; it
+  //   loses where most have not filled the window, one of 32k among 1k: 46.9 and 23.6).
   const bool brief = 1200 * tiles <= pairs * (350 + s.batch);
   const bool cut = w.window > 0 && 2 * tiles <= cap;
   const bool one_each = tiles <= 28 || brief || (cut && pairs >= 192) || pairs * tiles > 0x3fffffff;
